@@ -406,6 +406,161 @@ sbd_status sbd_profile_enable(sbd_ctx* ctx, int32_t enable);
 sbd_status sbd_stream_probe(void* stream, const void* buf, size_t bytes, uint32_t* sink);
 sbd_status sbd_profile_read(sbd_ctx* ctx, int32_t kernel, int32_t* launches, double* total_ms);
 
+/*
+ * ---------------------------------------------------------------------------------------
+ * Operators of an attention layer in 8-bit formats with a scale for each block, without a
+ * context: page tables of a serving batch, a paged e4m3 cache (written and read), and the
+ * e4m3 product of the projections around it with the quantiser that makes its operands.
+ *
+ * Conventions of these calls, besides the ones at the top of this file:
+ *  - stream is a hipStream_t of the current device (NULL = the null stream); every pointer
+ *    in the arguments and structs is device memory of that device unless it says host.  No
+ *    memory is allocated and nothing is copied to the host, so every call can be captured
+ *    into a HIP graph.  Two calls may run at once if neither writes what the other uses.
+ *  - Sequence lengths, tables and slots live on the device and are not checked on the host:
+ *    the kernels check every page id, slot and row against the sizes given here, so wrong
+ *    ones give wrong values (or rows left out), never an access outside the buffers.
+ *  - Errors are reported through sbd_last_error(NULL).
+ *  - Strides are in elements; a matrix or row named contiguous has none.
+ */
+/* Element types of 16- and 32-bit operands. */
+enum { SBD_TYPE_BF16 = 0, SBD_TYPE_FP16 = 1, SBD_TYPE_FP32 = 2 };
+
+/*
+ * Page tables of `batch` sequences that share n_pages pages of page_size tokens (a power of
+ * two from 16 to 256).  n_pages * page_size < 2^31 and max_pages * page_size <= 2^30.
+ *   table      [batch][max_pages]: the pages of each sequence, in order of position, then -1
+ *   held       [batch]: pages in each row of the table
+ *   cached     [batch]: tokens of each sequence that are cached (committed); the caller adds
+ *              to it, as sbd_commit does for the slots of a context
+ *   free_list  [n_pages], free_count [1]: the pages that no sequence holds, first free_count
+ *              entries; a permutation of all pages, and held = 0, to begin with
+ */
+typedef struct {
+  int32_t batch, max_pages, n_pages, page_size;
+  int32_t *table, *held, *cached, *free_list, *free_count;
+} sbd_page_table;
+
+/*
+ * The tables of the next step, in which sequence b adds n_new[b] rows after its cached ones.
+ *   n_new    [batch], 0 for a sequence that sits the step out
+ *   release  [batch] or NULL: where it is not 0 the sequence has ended.  Before anything
+ *            else its pages go back to the end of the free list (in order of sequence and
+ *            position), its table row becomes -1, held and cached 0; n_new[b] is then the
+ *            beginning of another sequence.
+ *   rows     rows that the step's tensors have (at least the sum of n_new; what is over is
+ *            padding)
+ * A sequence needs the pages that cover cached + n_new tokens and does not hold yet.
+ * Sequences are served in order: each gets all that it needs or nothing, and after the first
+ * that the free list cannot serve none that needs a page is served.  The pages taken are the
+ * last ones of the free list, in order.  A sequence of more than max_pages * page_size tokens
+ * or with a negative length is not served and takes nothing from others.
+ * Outputs: row_start [batch + 1] (rows of sequence b: row_start[b] .. row_start[b + 1], those
+ * of sequences that are not served too; a negative n_new counts as 0), kv_len [batch] (cached
+ * + n_new, or 0 where not served), slots [rows] (page * page_size + offset of each row's
+ * token; -1 for rows of a sequence that is not served and for padding).  table, held,
+ * free_list and free_count are updated; a sequence keeps the pages of rows that are not
+ * committed, for the next plan.
+ *   scratch  [3 * batch + 2], written before it is read
+ */
+sbd_status sbd_paged_plan(void* stream, const sbd_page_table* t, const int32_t* n_new, const uint8_t* release,
+                          int32_t rows, int32_t* row_start, int32_t* kv_len, int32_t* slots, int32_t* scratch);
+
+/*
+ * One layer's paged cache: e4m3 codes (SBD_KV_FP8_E4M3's) with a power of two for each page
+ * and KV head, keys and values apart: a value is e4m3(code) * 2^exp.
+ *   k_codes  [n_pages][n_kv_heads][page_size][head_dim]
+ *   v_codes  [n_pages][n_kv_heads][head_dim][page_size] (transposed: attention reads 16
+ *            tokens of one dimension at a time)
+ *   k_exp, v_exp  [n_pages][n_kv_heads], in [-100, 100]
+ * head_dim is 64 or 128; page_size as in sbd_page_table; codes 16-byte aligned.
+ */
+typedef struct {
+  int32_t n_pages, page_size, n_kv_heads, head_dim;
+  uint8_t *k_codes, *v_codes;
+  int8_t *k_exp, *v_exp;
+} sbd_paged_kv;
+
+/*
+ * Write a step's keys (after RoPE) and values into their pages.
+ *   k, v       SBD_TYPE_BF16 or _FP16 [rows][n_kv_heads][head_dim], rows k_stride / v_stride
+ *              elements apart (a multiple of 8; base 16-byte aligned)
+ *   row_start, slots  as sbd_paged_plan leaves them for this step
+ * Per page and head: e is the smallest whole number in [-100, 100] with |x| <= 448 * 2^e for
+ * every finite x written, and not below the page's exponent where the page keeps earlier
+ * tokens of the sequence (those before the first row written); where it grows, the kept codes
+ * are rounded again to the new scale.  Codes are the nearest e4m3 values, ties to even; what
+ * exceeds 448 * 2^e (infinities) saturates, NaN stays NaN.  Codes behind the last row written
+ * are left as they were.  Rows with a slot outside the cache, and padding, are left out.  No
+ * two sequences of a step may write into one page.
+ */
+sbd_status sbd_paged_append(void* stream, const sbd_paged_kv* c, int32_t dtype, int32_t batch, int32_t rows,
+                            const int32_t* row_start, const int32_t* slots, const void* k, int64_t k_stride,
+                            const void* v, int64_t v_stride);
+
+/*
+ * Attention of a step's rows over the paged cache (which holds the step's own rows already).
+ *   q, out     SBD_TYPE_BF16 or _FP16 [rows][n_q_heads][head_dim], rows q_stride / out_stride
+ *              elements apart (a multiple of 8; bases 16-byte aligned).  n_q_heads is a
+ *              multiple of n_kv_heads; query head h reads KV head h / (n_q_heads / n_kv_heads).
+ *   row_start, kv_len  as sbd_paged_plan leaves them
+ *   table      [batch][max_pages]; a position whose entry is outside [0, n_pages) is seen by
+ *              no row
+ *   n_causal   [batch] or NULL.  Row j of sequence b is the token at position
+ *              kv_len[b] - n_new[b] + j and sees the keys up to itself if j < n_causal[b],
+ *              else all kv_len[b] keys (the block-hybrid mask of sbd_block_forward).  NULL:
+ *              every row is causal.
+ *   scale      of the products q.k, finite
+ *   max_kv     what the longest kv_len is about, in [1, max_pages * page_size]: it decides
+ *              how the keys are split over the chip, not the result beyond summation order
+ * out = sum_i softmax_i(scale * q.k_i) v_i over the keys a row sees; a row that sees no key
+ * (its sequence was not served) gets zeros.  Sums and softmax statistics are fp32; a key
+ * whose weight is below 2^-39 of the row's largest may count as zero.  Values of keys that a
+ * row does not see never reach it, NaN included.  Rows behind row_start[batch] are left as
+ * they were.
+ *   workspace  sbd_paged_attention_workspace() bytes, 16-byte aligned (NULL if that is 0),
+ *              used by this call alone until it has ended
+ */
+sbd_status sbd_paged_attention_workspace(const sbd_paged_kv* c, int32_t batch, int32_t rows, int32_t n_q_heads,
+                                         int32_t max_kv, size_t* bytes);
+sbd_status sbd_paged_attention(void* stream, const sbd_paged_kv* c, int32_t dtype, int32_t batch, int32_t rows,
+                               int32_t n_q_heads, const int32_t* row_start, const int32_t* kv_len,
+                               const int32_t* table, int32_t max_pages, const int32_t* n_causal, float scale,
+                               int32_t max_kv, const void* q, int64_t q_stride, void* out, int64_t out_stride,
+                               void* workspace, size_t workspace_bytes);
+
+/*
+ * e4m3 codes of a matrix with a power of two for each block of block_rows x 128 elements
+ * (block_rows 1: activations; 128: weights): scale = 2^e, e the smallest whole number in
+ * [-100, 100] with |x| <= 448 * 2^e for every finite x of the block; code = the e4m3 value
+ * nearest to x / scale (ties to even, saturating, NaN stays NaN).
+ *   x       SBD_TYPE_* [rows][cols], rows x_stride elements apart; cols a multiple of 16, rows
+ *           16-byte aligned
+ *   codes   [rows][cols], contiguous, 16-byte aligned
+ *   scales  float, block_rows 1: [ceil(cols / 128)][rows] (the scales of one block of columns
+ *           lie together); block_rows 128: [ceil(rows / 128)][ceil(cols / 128)]
+ */
+sbd_status sbd_scaled_quantize(void* stream, int32_t dtype, int32_t rows, int32_t cols, const void* x,
+                               int64_t x_stride, int32_t block_rows, uint8_t* codes, float* scales);
+
+/*
+ * Product of e4m3 matrices with a scale for each block of 128 along K:
+ *   out[m][n] = sum_c a_scale[c][m] * b_scale[n / 128][c] * sum_{k in [128 c, 128 c + 128)} a[m][k] * b[n][k]
+ *   a        e4m3 codes [m][k], rows a_stride elements apart (a multiple of 16; 16-byte aligned)
+ *   a_scale  float [ceil(k / 128)][m] (any values)
+ *   b        e4m3 codes [n][k], contiguous, 16-byte aligned (the weights, [out][in])
+ *   b_scale  float [ceil(n / 128)][ceil(k / 128)] (any values)
+ *   k        a multiple of 16
+ *   out      SBD_TYPE_* [m][n], rows out_stride elements apart, aligned to its type
+ * The sums are fp32; out is rounded once.
+ *   workspace  sbd_scaled_matmul_workspace() bytes, 16-byte aligned (NULL if that is 0), used
+ *              by this call alone until it has ended
+ */
+sbd_status sbd_scaled_matmul_workspace(int32_t m, int32_t n, int32_t k, size_t* bytes);
+sbd_status sbd_scaled_matmul(void* stream, int32_t m, int32_t n, int32_t k, const uint8_t* a, int64_t a_stride,
+                             const float* a_scale, const uint8_t* b, const float* b_scale, int32_t out_type,
+                             void* out, int64_t out_stride, void* workspace, size_t workspace_bytes);
+
 const char* sbd_status_string(sbd_status s);
 /* Reason for the last failed call on ctx; ctx == NULL gives the calling thread's last
  * context-less failure (e.g. of sbd_create). */

@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, c_char_p, c_double, c_float, c_int32, c_size_t, c_void_p
+from ctypes import POINTER, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_void_p
 from typing import Optional
 
 import numpy as np
@@ -61,6 +61,17 @@ SIGNATURES = {
     "sbd_xcd_map_ok": [c_void_p, POINTER(c_int32)],
     "sbd_xcd_map_check": [c_void_p, c_int32, c_int32, POINTER(c_int32)],
     "sbd_stream_probe": [c_void_p, c_void_p, c_size_t, c_void_p],
+    "sbd_paged_plan": [c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_void_p],
+    "sbd_paged_append": [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_int64,
+                         c_void_p, c_int64],
+    "sbd_paged_attention_workspace": [c_void_p, c_int32, c_int32, c_int32, c_int32, POINTER(c_size_t)],
+    "sbd_paged_attention": [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p,
+                            c_int32, c_void_p, c_float, c_int32, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
+                            c_size_t],
+    "sbd_scaled_quantize": [c_void_p, c_int32, c_int32, c_int32, c_void_p, c_int64, c_int32, c_void_p, c_void_p],
+    "sbd_scaled_matmul_workspace": [c_int32, c_int32, c_int32, POINTER(c_size_t)],
+    "sbd_scaled_matmul": [c_void_p, c_int32, c_int32, c_int32, c_void_p, c_int64, c_void_p, c_void_p, c_void_p,
+                          c_int32, c_void_p, c_int64, c_void_p, c_size_t],
     "sbd_profile_read": [c_void_p, c_int32, POINTER(c_int32), POINTER(c_double)],
     "sbd_status_string": [c_int32],
     "sbd_last_error": [c_void_p],
@@ -79,6 +90,19 @@ class ModelConfig(ctypes.Structure):
 class Weights(ctypes.Structure):
     _fields_ = [("embed", c_void_p), ("lm_head", c_void_p), ("final_norm", c_void_p)] + \
                [(f, POINTER(c_void_p)) for f in LAYER_FIELDS] + [("fp8_scale_exp", POINTER(c_int32))]
+
+class PageTableArgs(ctypes.Structure):
+    """sbd_page_table"""
+    _fields_ = [("batch", c_int32), ("max_pages", c_int32), ("n_pages", c_int32), ("page_size", c_int32),
+                ("table", c_void_p), ("held", c_void_p), ("cached", c_void_p), ("free_list", c_void_p),
+                ("free_count", c_void_p)]
+
+
+class PagedKVArgs(ctypes.Structure):
+    """sbd_paged_kv"""
+    _fields_ = [("n_pages", c_int32), ("page_size", c_int32), ("n_kv_heads", c_int32), ("head_dim", c_int32),
+                ("k_codes", c_void_p), ("v_codes", c_void_p), ("k_exp", c_void_p), ("v_exp", c_void_p)]
+
 
 WEIGHT_FORMATS = {"bf16": 0, "fp8_e4m3": 1}  # SBD_WEIGHTS_*
 KV_FORMATS = {"bf16": 0, "fp8_e4m3": 1}      # SBD_KV_*

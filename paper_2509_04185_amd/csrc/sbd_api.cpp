@@ -13,6 +13,7 @@
 #include <string>
 #include <vector>
 
+#include "ops_internal.h"
 #include "sbd_internal.h"
 
 using namespace sbd;
@@ -206,6 +207,21 @@ sbd_status fail(sbd_ctx* c, sbd_status st, const char* fmt, ...) {
   if (c) c->err = buf; else g_err = buf;
   return st;
 }
+
+}  // namespace
+
+// The same for calls without a context whose checks are in another file (ops_api.cpp).
+sbd_status sbd::op_fail(sbd_status st, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  g_err = buf;
+  return st;
+}
+
+namespace {
 
 #define SBD_HIP(ctx, expr)                                                                  \
   do {                                                                                      \
