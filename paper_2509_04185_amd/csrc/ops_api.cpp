@@ -15,6 +15,7 @@ namespace {
 constexpr int32_t kMaxOpBatch = 1 << 16;
 constexpr int32_t kMaxOpRows = 1 << 24;
 constexpr int32_t kMaxOpHeads = 1024;
+constexpr int32_t kMaxOpDepth = 1 << 22;  // bytes of a row of codes: 256 rows lie within 32-bit offsets
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
@@ -85,8 +86,9 @@ sbd_status check_attention(const sbd_paged_kv* c, bool pointers, int32_t batch, 
 sbd_status check_matmul(int32_t m, int32_t n, int32_t k) {
   if (m < 0 || m > kMaxOpRows) return op_fail(SBD_ERR_INVALID_ARG, "m %d out of [0, %d]", m, kMaxOpRows);
   if (n < 1 || n > kMaxOpRows) return op_fail(SBD_ERR_INVALID_ARG, "n %d out of [1, %d]", n, kMaxOpRows);
-  if (k < 16 || k % 16 || k > kMaxOpRows)
-    return op_fail(SBD_ERR_INVALID_ARG, "k %d is no multiple of 16 in [16, %d]", k, kMaxOpRows);
+  if (k < 16 || k % 16 || k > kMaxOpDepth)
+    return op_fail(SBD_ERR_INVALID_ARG, "k %d is no multiple of 16 in [16, %d]", k, kMaxOpDepth);
+  if ((int64_t)m * n > ((int64_t)1 << 36)) return op_fail(SBD_ERR_INVALID_ARG, "m * n exceeds 2^36");
   return SBD_OK;
 }
 
@@ -202,8 +204,9 @@ sbd_status sbd_scaled_matmul(void* stream, int32_t m, int32_t n, int32_t k, cons
   if (m == 0) return SBD_OK;
   if (!a || !a_scale || !b || !b_scale || !out) return op_fail(SBD_ERR_INVALID_ARG, "null argument");
   if (!aligned16(a) || !aligned16(b)) return op_fail(SBD_ERR_INVALID_ARG, "a and b must be 16-byte aligned");
-  if (a_stride < k || a_stride % 16)
-    return op_fail(SBD_ERR_INVALID_ARG, "a row stride of %lld (need a multiple of 16 of at least %d)", (long long)a_stride, k);
+  if (a_stride < k || a_stride % 16 || a_stride > kMaxOpDepth)
+    return op_fail(SBD_ERR_INVALID_ARG, "a row stride of %lld (need a multiple of 16 in [%d, %d])", (long long)a_stride, k,
+                   kMaxOpDepth);
   if (out_stride < n) return op_fail(SBD_ERR_INVALID_ARG, "an output row stride of %lld, below n %d", (long long)out_stride, n);
   if (reinterpret_cast<uintptr_t>(out) % (out_type == SBD_TYPE_FP32 ? 4 : 2))
     return op_fail(SBD_ERR_INVALID_ARG, "out is not aligned to its type");

@@ -138,17 +138,25 @@ def attend(q, k_codes, v_codes, k_exp, v_exp, table, starts, kv_len, n_causal, s
 
 def matmul(a, a_scale, b, b_scale, out_type):
     """(out, bound) of the block-scaled product: fp32 sums of exact products, 128 and then one for
-    each block, two roundings for the scales, one rounding of the result."""
+    each block, two roundings for the scales, one rounding of the result.  The matrix instruction
+    of the 16-bit outputs cuts each of eight neighbouring products off at 2^-13 of the power of
+    two of the largest (at most the largest itself): 8 * 2^-13 of the largest for each group."""
     A, B = VALUES[a], VALUES[b]
     (m, k), n = A.shape, B.shape[0]
     kb = -(-k // 128)
-    out, size = np.zeros((m, n)), np.zeros((m, n))
+    out, size, cut = np.zeros((m, n)), np.zeros((m, n)), np.zeros((m, n))
     for c in range(kb):
         s = slice(128 * c, min(k, 128 * c + 128))
         f = a_scale[c].astype(np.float64)[:, None] * b_scale[:, c].astype(np.float64)[np.arange(n) // 128]
         out += (A[:, s] @ B[:, s].T) * f
         size += (np.abs(A[:, s]) @ np.abs(B[:, s]).T) * np.abs(f)
-    bound = size * (128 + kb + 4) * 2.0 ** -24 + HALF_STEP[out_type] * np.abs(out) * 1.01
+        if out_type != torch.float32:
+            for i in range(s.start, s.stop, 8):
+                top = np.zeros((m, n))
+                for j in range(i, min(i + 8, s.stop)):
+                    np.maximum(top, np.abs(A[:, j])[:, None] * np.abs(B[:, j])[None, :], out=top)
+                cut += top * 2.0 ** -10 * np.abs(f)
+    bound = cut + size * (128 + kb + 4) * 2.0 ** -24 + HALF_STEP[out_type] * np.abs(out) * 1.01
     top = float(torch.finfo(out_type).max)  # what exceeds the type is infinite in it
     return np.where(np.abs(out) > top, np.copysign(np.inf, out), out), bound
 

@@ -140,6 +140,7 @@ def test_matmul_refusals(lib):
                      (dict(k=8), "k "), (dict(t=3), "type"), (dict(a=None), "null"), (dict(a_s=None), "null"),
                      (dict(b=None), "null"), (dict(b_s=None), "null"), (dict(out=None), "null"), (dict(a=A + 8), "aligned"),
                      (dict(b=A + 4), "aligned"), (dict(sa=240), "stride"), (dict(sa=264), "stride"), (dict(so=255), "stride"),
+                     (dict(k=2 ** 22 + 16), "k "), (dict(sa=2 ** 22 + 16), "stride"), (dict(m=2 ** 20, n=2 ** 16 + 1), "2^36"),
                      (dict(out=A + 1), "aligned"), (dict(out=A + 2, t=2), "aligned")):
         refused(lib, INVALID, call(**kw), text)
     assert call(m=0, a=None, out=None) == 0
