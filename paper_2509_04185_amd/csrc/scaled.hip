@@ -236,15 +236,17 @@ __global__ __launch_bounds__(64 * kSkinnyWaves, 2) void skinny_kernel(MatmulArgs
   }
 }
 
-// More rows: tiles of 16 MT MW rows x 16 NT NW columns, MW x NW waves.  The rows' codes go
-// through LDS (every column's wave reads them), copied there straight from memory into one of
-// two buffers while the other is multiplied; a wave's weights come straight into its registers,
-// a block ahead.  LDS holds rows of 128 bytes whose 16-byte pieces are XOR-swizzled with the
-// row, so that the 16 rows of a fragment read spread over all banks.
+// More rows: tiles of 16 MT MW rows x 16 NT NW columns, MW x NW waves.  The codes of both go
+// through LDS, copied there straight from memory into one of two buffers while the other is
+// multiplied.  (A wave's weights straight into its registers would save a third of the LDS
+// reads, but a fragment's neighbouring lanes lie in different rows, so the vector cache is
+// asked for 16 bytes at a time: 4096 x 28672 x 4096 took 700 us that way.)  LDS holds rows of
+// 128 bytes whose 16-byte pieces are XOR-swizzled with the row, so that the 16 rows of a
+// fragment read spread over all banks.
 //
 // The copies are written as assembly without results: the compiler would otherwise wait for
-// every copy in flight before each read of LDS.  A wave waits for all of its loads once a
-// block, before the barrier.
+// every copy in flight before each read of LDS.  A wave waits for its copies once a block,
+// before the barrier.
 __device__ __forceinline__ void copy16_to_lds(__amdgpu_buffer_rsrc_t rsrc, uint32_t lds, uint32_t voff, uint32_t soff) {
   asm volatile(
       "s_mov_b32 m0, %0\n\t"
@@ -269,8 +271,8 @@ template <int MT, int NT, int MW, int NW>
 struct TileShape {
   static constexpr int kWaves = MW * NW, kThreads = 64 * kWaves;
   static constexpr int BM = 16 * MT * MW, BN = 16 * NT * NW;
-  static constexpr int kCopies = BM / 8 / kWaves;  // 1 KB copies (8 rows) of a wave and block
-  static_assert(kCopies * 8 * kWaves == BM, "whole copies");
+  static constexpr int kCopies = (BM + BN) / 8 / kWaves;  // 1 KB copies (8 rows) of a wave and block
+  static_assert(kCopies * 8 * kWaves == BM + BN && BM % (8 * kWaves) == 0, "whole copies, of one operand each");
 };
 
 template <class T, int MT, int NT, int MW, int NW, bool SPLIT>
@@ -278,7 +280,7 @@ __global__ __launch_bounds__(64 * MW * NW, MW * NW >= 8 ? 1 : 2) void tile_kerne
                                                                                  int blocks_per_split) {
   using S = TileShape<MT, NT, MW, NW>;
   constexpr bool WIDE = std::is_same_v<T, float>;
-  __shared__ __attribute__((aligned(1024))) uint8_t s_x[2][S::BM * 128];
+  __shared__ __attribute__((aligned(1024))) uint8_t s_x[2][(S::BM + S::BN) * 128];  // rows, then weights
   __shared__ float s_s[2][S::BM];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, grp = lane >> 4;
   const int mw = w % MW, nw = w / MW;
@@ -297,34 +299,29 @@ __global__ __launch_bounds__(64 * MW * NW, MW * NW >= 8 ? 1 : 2) void tile_kerne
   const int m0 = tm * S::BM, n0 = tn * S::BN;
   const int c0 = SPLIT ? blockIdx.y * blocks_per_split : 0, c1 = SPLIT ? min(c0 + blocks_per_split, kb) : kb;
 
-  // Copies of the rows' codes: lane l brings piece (l % 8) ^ (l / 8) of row l / 8.  Each wave
-  // also brings the scales of 64 rows (some waves the same ones).
-  const __amdgpu_buffer_rsrc_t rx = buf_rsrc(a.a + m0 * a.a_stride);
-  uint32_t xoff[S::kCopies];
+  // Copies: lane l brings piece (l % 8) ^ (l / 8) of row l / 8 of eight.  Each wave also brings
+  // the scales of 64 rows (some waves the same ones).
+  constexpr int kRowCopies = S::BM / 8 / S::kWaves;
+  const __amdgpu_buffer_rsrc_t rx = buf_rsrc(a.a + m0 * a.a_stride), rw = buf_rsrc(a.b + (int64_t)n0 * a.k);
+  uint32_t off[S::kCopies];
   const uint32_t piece = ((lane & 7) ^ (lane >> 3)) * 16;
 #pragma unroll
   for (int u = 0; u < S::kCopies; ++u) {
-    const int row = 8 * (w + S::kWaves * u) + (lane >> 3);
-    xoff[u] = (uint32_t)min(row, a.m - 1 - m0) * (uint32_t)a.a_stride + piece;
+    const int row = 8 * (w + S::kWaves * (u < kRowCopies ? u : u - kRowCopies)) + (lane >> 3);
+    off[u] = (u < kRowCopies ? (uint32_t)min(row, a.m - 1 - m0) * (uint32_t)a.a_stride
+                             : (uint32_t)min(row, a.n - 1 - n0) * (uint32_t)a.k) + piece;
   }
   const int srow = w % (S::BM / 64) * 64;
   const uint32_t soff = (uint32_t)min(m0 + srow + lane, a.m - 1) * 4;
-  auto copy_rows = [&](int c, int buf, auto tail) {
+  auto copy_block = [&](int c, int buf, auto tail) {
     const uint32_t lds = lds_addr(s_x[buf]) + w * 1024;
     // in the last block, pieces behind its end are read from inside the row (and not used)
     const uint32_t over = tail ? (uint32_t)max(0, (int)(128 * c + piece) - (a.k - 16)) : 0;
 #pragma unroll
     for (int u = 0; u < S::kCopies; ++u)
-      copy16_to_lds(rx, __builtin_amdgcn_readfirstlane(lds + u * S::kWaves * 1024), xoff[u] - over, 128 * c);
+      copy16_to_lds(u < kRowCopies ? rx : rw, __builtin_amdgcn_readfirstlane(lds + u * S::kWaves * 1024), off[u] - over, 128 * c);
     copy4_to_lds(buf_rsrc(a.a_scale + (int64_t)c * a.m), __builtin_amdgcn_readfirstlane(lds_addr(s_s[buf]) + srow * 4), soff, 0);
   };
-
-  const __amdgpu_buffer_rsrc_t rw = buf_rsrc(a.b + (int64_t)(n0 + 16 * NT * nw) * a.k);
-  uint32_t woff[NT];
-#pragma unroll
-  for (int i = 0; i < NT; ++i) woff[i] = (uint32_t)max(0, min(16 * i + r, a.n - 1 - n0 - 16 * NT * nw)) * (uint32_t)a.k + 16 * grp;
-  const bool any_cols = n0 + 16 * NT * nw < a.n;  // else the wave multiplies rows of another, and stores nothing
-  const __amdgpu_buffer_rsrc_t rwv = any_cols ? rw : buf_rsrc(a.b);
   const float* sb = a.b_scale + (int64_t)min((n0 + 16 * NT * nw) / 128, (a.n - 1) / 128) * kb;
 
   f32x4 acc[NT][MT];
@@ -333,42 +330,55 @@ __global__ __launch_bounds__(64 * MW * NW, MW * NW >= 8 ? 1 : 2) void tile_kerne
 #pragma unroll
     for (int j = 0; j < MT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  const uint32_t frag0 = (16 * MT * mw + r) * 128 + ((grp ^ (r & 7)) * 16);
-  i32x8 wf[NT];
-  float sbf;
+  const uint32_t swz = (grp ^ (r & 7)) * 16;
+  const uint32_t frag_x = (16 * MT * mw + r) * 128 + swz, frag_w = (S::BM + 16 * NT * nw + r) * 128 + swz;
   // A fragment piece of the last block is there if it is not behind its end; pieces are whole.
   const bool lo_in = 128 * (kb - 1) + 16 * grp < a.k, hi_in = 128 * (kb - 1) + 64 + 16 * grp < a.k;
   const i32x4 zero{0, 0, 0, 0};
-  auto load_weights = [&](int c, i32x8 (&f)[NT], float& s, auto tail) {
-#pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      if (tail)
-        f[i] = join8(lo_in ? __builtin_amdgcn_raw_buffer_load_b128(rwv, woff[i], 128 * c, 0) : zero,
-                     hi_in ? __builtin_amdgcn_raw_buffer_load_b128(rwv, woff[i] + 64, 128 * c, 0) : zero);
-      else
-        f[i] = join8(__builtin_amdgcn_raw_buffer_load_b128(rwv, woff[i], 128 * c, 0),
-                     __builtin_amdgcn_raw_buffer_load_b128(rwv, woff[i] + 64, 128 * c, 0));
+  auto read_frag = [&](int buf, uint32_t at, auto tail) {
+    i32x4 lo = *(const i32x4*)(s_x[buf] + at), hi = *(const i32x4*)(s_x[buf] + (at ^ 64));
+    if (tail) {
+      if (!lo_in) lo = zero;
+      if (!hi_in) hi = zero;
     }
-    s = sb[c];
+    return join8(lo, hi);
   };
-  auto step = [&](int buf, const i32x8 (&f)[NT], float s, auto tail) {
+  // The products of a fragment are issued one after the other; while one runs, the sums take in
+  // the one before it and the next fragment is read.
+  auto step = [&](int buf, float s, auto tail) {
+    i32x8 f[NT];
+    i32x8 x = read_frag(buf, frag_x, tail), x_next = x;
+    float scale = s_s[buf][16 * MT * mw + r], scale_next = 0.f;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) f[i] = read_frag(buf, frag_w + 2048 * i, tail);
+    f32x4 before;
+    float before_scale = 0.f;
 #pragma unroll
     for (int j = 0; j < MT; ++j) {
-      i32x4 lo = *(const i32x4*)(s_x[buf] + frag0 + 2048 * j), hi = *(const i32x4*)(s_x[buf] + (frag0 ^ 64) + 2048 * j);
-      const float f0 = s_s[buf][16 * (MT * mw + j) + r] * s;
-      if (tail) {
-        if (!lo_in) lo = zero;
-        if (!hi_in) hi = zero;
+      if (j + 1 < MT) {
+        x_next = read_frag(buf, frag_x + 2048 * (j + 1), tail);
+        scale_next = s_s[buf][16 * (MT * mw + j + 1) + r];
       }
-      const i32x8 x = join8(lo, hi);
+      const float f0 = scale * s;
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
         const f32x4 p = block_product<WIDE>(f[i], x);
+        __builtin_amdgcn_sched_barrier(0);
+        const int was = j * NT + i - 1;
+        if (was >= 0) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) acc[i][j][q] = __builtin_fmaf(p[q], f0, acc[i][j][q]);
+          for (int q = 0; q < 4; ++q)
+            acc[was % NT][was / NT][q] = __builtin_fmaf(before[q], before_scale, acc[was % NT][was / NT][q]);
+        }
+        before = p;
+        before_scale = f0;
+        __builtin_amdgcn_sched_barrier(0);
       }
-      if constexpr (MT == 8) __builtin_amdgcn_sched_barrier(0);  // more fragments at once do not fit the registers
+      x = x_next;
+      scale = scale_next;
     }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) acc[NT - 1][MT - 1][q] = __builtin_fmaf(before[q], before_scale, acc[NT - 1][MT - 1][q]);
   };
   auto wait_all = [] {
     asm volatile("" ::: "memory");
@@ -377,49 +387,80 @@ __global__ __launch_bounds__(64 * MW * NW, MW * NW >= 8 ? 1 : 2) void tile_kerne
     asm volatile("" ::: "memory");
   };
 
-  // Whole blocks two at a time (the last ones bring a block again that is not used).
+  // Whole blocks two at a time (the last one is brought again where there is no next).
   const std::integral_constant<bool, false> whole;
   const std::integral_constant<bool, true> part;
   const int cf = min(c1, a.k / 128);
   int c = c0;
+  float sbf = 0.f;
   if (c < cf) {
-    copy_rows(c, 0, whole);
-    load_weights(c, wf, sbf, whole);
+    copy_block(c, 0, whole);
+    sbf = sb[c];
   }
   for (; c + 2 <= cf; c += 2) {
-    i32x8 wg[NT];
-    float sbg;
     wait_all();
-    copy_rows(c + 1, 1, whole);
-    load_weights(c + 1, wg, sbg, whole);
-    step(0, wf, sbf, whole);
+    copy_block(c + 1, 1, whole);
+    const float sbg = sb[c + 1];
+    step(0, sbf, whole);
     wait_all();
     const int next = min(c + 2, cf - 1);
-    copy_rows(next, 0, whole);
-    load_weights(next, wf, sbf, whole);
-    step(1, wg, sbg, whole);
+    copy_block(next, 0, whole);
+    sbf = sb[next];
+    step(1, sbg, whole);
   }
   wait_all();
-  if (c < cf) step(0, wf, sbf, whole);
+  if (c < cf) step(0, sbf, whole);
   if (cf < c1) {
-    copy_rows(cf, 1, part);
-    load_weights(cf, wf, sbf, part);
+    copy_block(cf, 1, part);
+    sbf = sb[cf];
     wait_all();
-    step(1, wf, sbf, part);
+    step(1, sbf, part);
   }
 
-  const bool vec = vec_ok<T>(a);
+  // Each wave turns its sums around in a part of LDS of its own, so that it stores whole lines:
+  // 8-byte pieces of 16 rows straight from the registers cost 31 us a 256 x 256 tile.
+  using E = std::conditional_t<SPLIT, float, T>;
+  constexpr int ES = std::is_same_v<E, float> ? 4 : 2, kWidth = 16 * NT * ES, kPieces = kWidth / 16;
+  static_assert(S::BM * S::BN * ES <= (int)sizeof(s_x), "the sums fit the buffers");
+  __syncthreads();  // every wave is done with the buffers
+  uint8_t* turn = &s_x[0][0] + w * 16 * MT * kWidth;
 #pragma unroll
   for (int j = 0; j < MT; ++j) {
-    const int row = m0 + 16 * (MT * mw + j) + r;
-    if (row >= a.m) continue;
+    const int row = 16 * j + r;
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-      const int n = n0 + 16 * (NT * nw + i) + 4 * grp;
-      if constexpr (SPLIT)
-        store4<float>(a.part, ((int64_t)blockIdx.y * a.m + row) * a.n + n, a.n - n, a.n % 4 == 0, acc[i][j]);
+      const int byte = (16 * i + 4 * grp) * ES, at = row * kWidth + (((byte / 16) ^ (row % kPieces)) * 16) + byte % 16;
+      const f32x4 v = acc[i][j];
+      if constexpr (ES == 4)
+        *(f32x4*)(turn + at) = v;
       else
-        store4<T>(a.out, row * a.out_stride + n, a.n - n, vec, acc[i][j]);
+        *(i32x2*)(turn + at) = i32x2{(int)pack2<E>(v[0], v[1]), (int)pack2<E>(v[2], v[3])};
+    }
+  }
+  __builtin_amdgcn_s_waitcnt((15 | (3 << 14)) | (7 << 4));  // lgkmcnt(0): only this wave reads what it wrote
+  asm volatile("" ::: "memory");
+  uint8_t* out = static_cast<uint8_t*>(SPLIT ? static_cast<void*>(a.part + (int64_t)blockIdx.y * a.m * a.n) : a.out);
+  const int64_t stride = SPLIT ? a.n : a.out_stride;
+  const bool vec = stride * ES % 16 == 0 && (uintptr_t)out % 16 == 0;
+  constexpr int kRows = 64 / kPieces, kEls = 16 / ES;
+  const int p = lane % kPieces, n = n0 + 16 * NT * nw + p * kEls;
+#pragma unroll
+  for (int u = 0; u < 16 * MT / kRows; ++u) {
+    const int row = u * kRows + lane / kPieces, m = m0 + 16 * MT * mw + row;
+    const i32x4 v = *(const i32x4*)(turn + row * kWidth + ((p ^ (row % kPieces)) * 16));
+    if (m >= a.m || n >= a.n) continue;
+    uint8_t* at = out + (m * stride + n) * ES;
+    if (vec && n + kEls <= a.n) {
+      *(i32x4*)at = v;
+    } else {
+#pragma unroll
+      for (int e = 0; e < kEls; ++e) {
+        if (n + e >= a.n) break;
+        if constexpr (ES == 4)
+          *(int*)(at + 4 * e) = v[e];
+        else
+          *(uint16_t*)(at + 2 * e) = (uint16_t)((uint32_t)v[e / 2] >> (16 * (e % 2)));
+      }
     }
   }
 }
