@@ -280,8 +280,9 @@ __global__ __launch_bounds__(64 * MW * NW, MW * NW >= 8 ? 1 : 2) void tile_kerne
                                                                                  int blocks_per_split) {
   using S = TileShape<MT, NT, MW, NW>;
   constexpr bool WIDE = std::is_same_v<T, float>;
-  __shared__ __attribute__((aligned(1024))) uint8_t s_x[2][(S::BM + S::BN) * 128];  // rows, then weights
-  __shared__ float s_s[2][S::BM];
+  // 1 KB pieces of 8 rows, the two buffers' in turn; rows, then weights
+  __shared__ __attribute__((aligned(1024))) uint8_t s_x[(S::BM + S::BN) * 256];
+  __shared__ float s_s[2][S::BM], s_b[2][S::kWaves][64];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, grp = lane >> 4;
   const int mw = w % MW, nw = w / MW;
   const int kb = (a.k + 127) / 128;
@@ -299,30 +300,38 @@ __global__ __launch_bounds__(64 * MW * NW, MW * NW >= 8 ? 1 : 2) void tile_kerne
   const int m0 = tm * S::BM, n0 = tn * S::BN;
   const int c0 = SPLIT ? blockIdx.y * blocks_per_split : 0, c1 = SPLIT ? min(c0 + blocks_per_split, kb) : kb;
 
-  // Copies: lane l brings piece (l % 8) ^ (l / 8) of row l / 8 of eight.  Each wave also brings
-  // the scales of 64 rows (some waves the same ones).
+  // Copies: lane l brings piece (l % 8) ^ (l / 8) of row l / 8 of eight.  Rows behind the last
+  // one are outside the buffer's range by the lane's own offset (row * stride is at least its
+  // size): the hardware does not read them, and what stands for them is not stored.  Each wave also brings the scales of 64 rows (some waves the same ones) and the
+  // weights' scale of its columns.
   constexpr int kRowCopies = S::BM / 8 / S::kWaves;
-  const __amdgpu_buffer_rsrc_t rx = buf_rsrc(a.a + m0 * a.a_stride), rw = buf_rsrc(a.b + (int64_t)n0 * a.k);
-  uint32_t off[S::kCopies];
-  const uint32_t piece = ((lane & 7) ^ (lane >> 3)) * 16;
-#pragma unroll
-  for (int u = 0; u < S::kCopies; ++u) {
-    const int row = 8 * (w + S::kWaves * (u < kRowCopies ? u : u - kRowCopies)) + (lane >> 3);
-    off[u] = (u < kRowCopies ? (uint32_t)min(row, a.m - 1 - m0) * (uint32_t)a.a_stride
-                             : (uint32_t)min(row, a.n - 1 - n0) * (uint32_t)a.k) + piece;
-  }
-  const int srow = w % (S::BM / 64) * 64;
-  const uint32_t soff = (uint32_t)min(m0 + srow + lane, a.m - 1) * 4;
-  auto copy_block = [&](int c, int buf, auto tail) {
-    const uint32_t lds = lds_addr(s_x[buf]) + w * 1024;
-    // in the last block, pieces behind its end are read from inside the row (and not used)
-    const uint32_t over = tail ? (uint32_t)max(0, (int)(128 * c + piece) - (a.k - 16)) : 0;
-#pragma unroll
-    for (int u = 0; u < S::kCopies; ++u)
-      copy16_to_lds(u < kRowCopies ? rx : rw, __builtin_amdgcn_readfirstlane(lds + u * S::kWaves * 1024), off[u] - over, 128 * c);
-    copy4_to_lds(buf_rsrc(a.a_scale + (int64_t)c * a.m), __builtin_amdgcn_readfirstlane(lds_addr(s_s[buf]) + srow * 4), soff, 0);
+  auto rows_of = [](const uint8_t* p, int64_t rows, int64_t stride, int64_t width) {
+    const int64_t bytes = min((rows - 1) * stride + width, (int64_t)0x7fffffff);
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), (short)0, (int)bytes, 0x00020000);
   };
-  const float* sb = a.b_scale + (int64_t)min((n0 + 16 * NT * nw) / 128, (a.n - 1) / 128) * kb;
+  const __amdgpu_buffer_rsrc_t rx = rows_of(a.a + m0 * a.a_stride, min(a.m - m0, S::BM), a.a_stride, a.k);
+  const __amdgpu_buffer_rsrc_t rw = rows_of(a.b + (int64_t)n0 * a.k, min(a.n - n0, S::BN), a.k, a.k);
+  const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
+  const uint32_t off_x = (lane >> 3) * (uint32_t)a.a_stride + piece, off_w = (lane >> 3) * (uint32_t)a.k + piece;
+  const int srow = w % (S::BM / 64) * 64;
+  const uint32_t off_s = (uint32_t)min(m0 + srow + lane, a.m - 1) * 4;
+  const __amdgpu_buffer_rsrc_t rb = buf_rsrc(a.b_scale + (int64_t)min((n0 + 16 * NT * nw) / 128, (a.n - 1) / 128) * kb);
+  // Copies u0 .. u1 of a block (all of them: kCopies; the scales come with the first).
+  auto copy_some = [&](int c, int buf, auto tail, int u0, int u1) {
+    const uint32_t lds = lds_addr(s_x) + buf * 1024;
+    // in the last block, pieces behind its end are read from inside the row (and not used)
+    const uint32_t over = tail ? (uint32_t)max(0, 128 * c + piece - (a.k - 16)) : 0;
+#pragma unroll
+    for (int u = u0; u < u1; ++u) {
+      const int q = w + S::kWaves * u, row = 8 * (u < kRowCopies ? q : q - S::BM / 8);
+      const uint32_t at = (uint32_t)row * (uint32_t)(u < kRowCopies ? a.a_stride : a.k);
+      copy16_to_lds(u < kRowCopies ? rx : rw, __builtin_amdgcn_readfirstlane(lds + q * 2048),
+                    (u < kRowCopies ? off_x : off_w) - over + at, 128 * c);
+    }
+    if (u0 > 0) return;
+    copy4_to_lds(buf_rsrc(a.a_scale + (int64_t)c * a.m), __builtin_amdgcn_readfirstlane(lds_addr(s_s[buf]) + srow * 4), off_s, 0);
+    copy4_to_lds(rb, __builtin_amdgcn_readfirstlane(lds_addr(s_b[buf][w])), 0, 4 * c);
+  };
 
   f32x4 acc[NT][MT];
 #pragma unroll
@@ -330,39 +339,60 @@ __global__ __launch_bounds__(64 * MW * NW, MW * NW >= 8 ? 1 : 2) void tile_kerne
 #pragma unroll
     for (int j = 0; j < MT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  const uint32_t swz = (grp ^ (r & 7)) * 16;
-  const uint32_t frag_x = (16 * MT * mw + r) * 128 + swz, frag_w = (S::BM + 16 * NT * nw + r) * 128 + swz;
+  const uint32_t lane_at = (r >> 3) * 2048 + (r & 7) * 128 + (grp ^ (r & 7)) * 16;
+  const uint32_t frag_x = 2 * MT * mw * 2048 + lane_at, frag_w = (S::BM / 8 + 2 * NT * nw) * 2048 + lane_at;
   // A fragment piece of the last block is there if it is not behind its end; pieces are whole.
   const bool lo_in = 128 * (kb - 1) + 16 * grp < a.k, hi_in = 128 * (kb - 1) + 64 + 16 * grp < a.k;
   const i32x4 zero{0, 0, 0, 0};
-  auto read_frag = [&](int buf, uint32_t at, auto tail) {
-    i32x4 lo = *(const i32x4*)(s_x[buf] + at), hi = *(const i32x4*)(s_x[buf] + (at ^ 64));
+  auto read_frag = [&](uint32_t at, uint32_t more, auto tail) {
+    i32x4 lo = *(const i32x4*)(s_x + at + more), hi = *(const i32x4*)(s_x + (at ^ 64) + more);
     if (tail) {
       if (!lo_in) lo = zero;
       if (!hi_in) hi = zero;
     }
     return join8(lo, hi);
   };
-  // The products of a fragment are issued one after the other; while one runs, the sums take in
-  // the one before it and the next fragment is read.
-  auto step = [&](int buf, float s, auto tail) {
-    i32x8 f[NT];
-    i32x8 x = read_frag(buf, frag_x, tail), x_next = x;
-    float scale = s_s[buf][16 * MT * mw + r], scale_next = 0.f;
+  const std::integral_constant<bool, false> whole;
+  const std::integral_constant<bool, true> part;
+  auto wait_all = [] {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(7 << 4);  // vmcnt(0), lgkmcnt(0): this wave's copies have landed, its reads are done
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  // What a step begins with: the weights' fragments, the first row fragment and their scales.
+  struct Begin {
+    i32x8 f[NT], x;
+    float sx, sb;
+  };
+  auto read_begin = [&](int buf, Begin& b, auto tail) {
+    b.x = read_frag(frag_x, buf * 1024, tail);
+    b.sx = s_s[buf][16 * MT * mw + r];
+    b.sb = s_b[buf][w][0];
 #pragma unroll
-    for (int i = 0; i < NT; ++i) f[i] = read_frag(buf, frag_w + 2048 * i, tail);
+    for (int i = 0; i < NT; ++i) b.f[i] = read_frag(frag_w, buf * 1024 + 4096 * i, tail);
+  };
+  // One block.  The products of a fragment are issued one after the other; while one runs, the
+  // sums take in the one before it and the next fragment is read.  When the last row fragment
+  // is there (two fragments' products are still to come) turn() passes the barrier at which
+  // every wave is done with this buffer and the next block has landed in the other.
+  auto step = [&](int buf, const Begin& b, auto tail, auto&& fill, auto&& turn) {
+    i32x8 x = b.x, x_next = x;
+    float scale = b.sx, scale_next = 0.f;
     f32x4 before;
     float before_scale = 0.f;
 #pragma unroll
     for (int j = 0; j < MT; ++j) {
       if (j + 1 < MT) {
-        x_next = read_frag(buf, frag_x + 2048 * (j + 1), tail);
+        x_next = read_frag(frag_x, buf * 1024 + 4096 * (j + 1), tail);
         scale_next = s_s[buf][16 * (MT * mw + j + 1) + r];
       }
-      const float f0 = scale * s;
+      if (j < MT / 2) fill(j);
+      if (j == MT - 1) turn();
+      const float f0 = scale * b.sb;
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
-        const f32x4 p = block_product<WIDE>(f[i], x);
+        const f32x4 p = block_product<WIDE>(b.f[i], x);
         __builtin_amdgcn_sched_barrier(0);
         const int was = j * NT + i - 1;
         if (was >= 0) {
@@ -380,41 +410,40 @@ __global__ __launch_bounds__(64 * MW * NW, MW * NW >= 8 ? 1 : 2) void tile_kerne
 #pragma unroll
     for (int q = 0; q < 4; ++q) acc[NT - 1][MT - 1][q] = __builtin_fmaf(before[q], before_scale, acc[NT - 1][MT - 1][q]);
   };
-  auto wait_all = [] {
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(7 << 4);  // vmcnt(0), lgkmcnt(0): this wave's copies have landed, its reads are done
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-  };
 
-  // Whole blocks two at a time (the last one is brought again where there is no next).
-  const std::integral_constant<bool, false> whole;
-  const std::integral_constant<bool, true> part;
+  // Whole blocks (the last one is brought again where there is no next), then the last part.
+  // A block's copies are spread over the first half of the step before it: issued at once they
+  // fill the queue of the vector memory unit and every wave waits there.
   const int cf = min(c1, a.k / 128);
-  int c = c0;
-  float sbf = 0.f;
-  if (c < cf) {
-    copy_block(c, 0, whole);
-    sbf = sb[c];
-  }
-  for (; c + 2 <= cf; c += 2) {
+  if (c0 < cf) {
+    Begin b0, b1;
+    constexpr int kEach = (S::kCopies + MT / 2 - 1) / (MT / 2);
+    auto fill = [&](int c, int buf, int j) {
+      copy_some(min(c, cf - 1), buf, whole, min(kEach * j, S::kCopies), min(kEach * (j + 1), S::kCopies));
+    };
+    copy_some(c0, 0, whole, 0, S::kCopies);
     wait_all();
-    copy_block(c + 1, 1, whole);
-    const float sbg = sb[c + 1];
-    step(0, sbf, whole);
+    read_begin(0, b0, whole);
+    for (int c = c0;; c += 2) {
+      step(0, b0, whole, [&](int j) { fill(c + 1, 1, j); }, [&] {
+        wait_all();
+        read_begin(1, b1, whole);
+      });
+      if (c + 1 >= cf) break;
+      step(1, b1, whole, [&](int j) { fill(c + 2, 0, j); }, [&] {
+        wait_all();
+        read_begin(0, b0, whole);
+      });
+      if (c + 2 >= cf) break;
+    }
     wait_all();
-    const int next = min(c + 2, cf - 1);
-    copy_block(next, 0, whole);
-    sbf = sb[next];
-    step(1, sbg, whole);
   }
-  wait_all();
-  if (c < cf) step(0, sbf, whole);
   if (cf < c1) {
-    copy_block(cf, 1, part);
-    sbf = sb[cf];
+    Begin b;
+    copy_some(cf, 0, part, 0, S::kCopies);
     wait_all();
-    step(1, sbf, part);
+    read_begin(0, b, part);
+    step(0, b, part, [](int) {}, [] {});
   }
 
   // Each wave turns its sums around in a part of LDS of its own, so that it stores whole lines:
@@ -423,7 +452,7 @@ __global__ __launch_bounds__(64 * MW * NW, MW * NW >= 8 ? 1 : 2) void tile_kerne
   constexpr int ES = std::is_same_v<E, float> ? 4 : 2, kWidth = 16 * NT * ES, kPieces = kWidth / 16;
   static_assert(S::BM * S::BN * ES <= (int)sizeof(s_x), "the sums fit the buffers");
   __syncthreads();  // every wave is done with the buffers
-  uint8_t* turn = &s_x[0][0] + w * 16 * MT * kWidth;
+  uint8_t* turn = s_x + w * 16 * MT * kWidth;
 #pragma unroll
   for (int j = 0; j < MT; ++j) {
     const int row = 16 * j + r;

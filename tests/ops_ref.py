@@ -136,18 +136,19 @@ def attend(q, k_codes, v_codes, k_exp, v_exp, table, starts, kv_len, n_causal, s
     return out, bound
 
 
-def matmul(a, a_scale, b, b_scale, out_type):
+def matmul(a, a_scale, b, b_scale, out_type, cols=None):
     """(out, bound) of the block-scaled product: fp32 sums of exact products, 128 and then one for
     each block, two roundings for the scales, one rounding of the result.  The matrix instruction
     of the 16-bit outputs cuts each of eight neighbouring products off at 2^-13 of the power of
-    two of the largest (at most the largest itself): 8 * 2^-13 of the largest for each group."""
+    two of the largest (at most the largest itself): 8 * 2^-13 of the largest for each group.
+    cols: which columns of the whole product the rows of b are (their scales' blocks)."""
     A, B = VALUES[a], VALUES[b]
     (m, k), n = A.shape, B.shape[0]
     kb = -(-k // 128)
     out, size, cut = np.zeros((m, n)), np.zeros((m, n)), np.zeros((m, n))
     for c in range(kb):
         s = slice(128 * c, min(k, 128 * c + 128))
-        f = a_scale[c].astype(np.float64)[:, None] * b_scale[:, c].astype(np.float64)[np.arange(n) // 128]
+        f = a_scale[c].astype(np.float64)[:, None] * b_scale[:, c].astype(np.float64)[(np.arange(n) if cols is None else cols) // 128]
         out += (A[:, s] @ B[:, s].T) * f
         size += (np.abs(A[:, s]) @ np.abs(B[:, s]).T) * np.abs(f)
         if out_type != torch.float32:

@@ -120,6 +120,27 @@ def test_matmul_sizes_and_types(m, n, k, dtype):
     check_matmul(m, n, k, dtype, stride=32)
 
 
+@pytest.mark.parametrize("m,n,k,dtype", [(4096, 3600, 272, BF), (3500, 4100, 128, FP), (300, 28672, 656, BF),
+                                         (257, 49285, 144, BF), (1100, 4096, 400, F32)], ids=lambda v: str(v))
+def test_matmul_large(m, n, k, dtype):
+    """Products of many tiles: rows and columns around the tiles' ends against the plain form."""
+    from paper_2509_04185_amd import scaled_matmul
+    print(f"[gpu] scaled matmul {m} x {n} x {k} {dtype}", flush=True)
+    a, sa, b, sb = make(m, n, k, m, stride=16)
+    got = R.f64(scaled_matmul(a, sa, b, sb, out_dtype=dtype))
+    torch.cuda.synchronize()
+
+    def some(size):
+        near = np.concatenate([np.arange(e - 4, e + 4) for e in range(0, size + 257, 256)] + [np.arange(0, size, 37)])
+        return np.unique(near[(near >= 0) & (near < size)])[:700]
+    rows, cols = some(m), some(n)
+    rows, cols = rows[::max(1, len(rows) // 150)], np.concatenate([cols[:300], some(n)[-100:]])
+    want, bound = R.matmul(host(a)[rows], host(sa)[:, rows], host(b)[cols], host(sb), dtype, cols=cols)
+    share = R.worst(got[np.ix_(rows, cols)], want, bound)
+    print(f"    largest error {share:.3f} of its bound", flush=True)
+    assert share <= 1.0 and np.isfinite(got).all()
+
+
 @pytest.mark.parametrize("m", [9, 70, 300])
 def test_matmul_strided_output(m):
     """Rows of a wider, oddly aligned output: nothing beside them is written."""
