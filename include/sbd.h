@@ -515,7 +515,7 @@ sbd_status sbd_paged_append(void* stream, const sbd_paged_kv* c, int32_t dtype, 
  *              how the keys are split over the chip, not the result beyond summation order
  * out = sum_i softmax_i(scale * q.k_i) v_i over the keys a row sees; a row that sees no key
  * (its sequence was not served) gets zeros.  Sums and softmax statistics are fp32; a key
- * whose weight is below 2^-39 of the row's largest may count as zero.  Values of keys that a
+ * whose weight is below 2^-36 of the row's largest may count as zero.  Values of keys that a
  * row does not see never reach it, NaN included.  Rows behind row_start[batch] are left as
  * they were.
  *   workspace  sbd_paged_attention_workspace() bytes, 16-byte aligned (NULL if that is 0),

@@ -92,8 +92,9 @@ def append(codes, exps, x, starts, slots, page):
 def attend(q, k_codes, v_codes, k_exp, v_exp, table, starts, kv_len, n_causal, scale, page, out_type):
     """(out, bound): float64 attention of every row, and how far the kernel may be from it.
 
-    Bound, from the kernel's arithmetic: the weights are fp16, off by 2^-11 of themselves or by
-    the half step 2^-40 of the row's largest weight below the normal range; a score is a
+    Bound, from the kernel's arithmetic: the weights are fp16 and held as 2^11 times a power of
+    two that is at most the row's largest, so they are off by 2^-11 of themselves or by half of
+    fp16's smallest step, 2^-25 / 2^11 = 2^-36 of the row's largest; a score is a
     sum of dim exact products in fp32 (off by dim * 2^-24 of the sum of their sizes, and by two
     roundings of 2^-24 where it is scaled and the maximum is taken off), an exponential is off
     by 2^-22 of itself; the sums of weights and outputs are fp32 (each of N terms adds 2^-24 of
@@ -131,7 +132,7 @@ def attend(q, k_codes, v_codes, k_exp, v_exp, table, starts, kv_len, n_causal, s
                 out[starts[b] + j, h] = o
                 ds = size.max() * (dh + 3) * 2.0 ** -24 + np.abs(s).max() * 2.0 ** -23
                 rel = 2.0 ** -11 + 2 * ds + 2.0 ** -21 + (N + 70) * 2.0 ** -23
-                bound[starts[b] + j, h] = (rel * (w @ np.abs(vv)) + 2.0 ** -39 * np.abs(vv).sum(0)
+                bound[starts[b] + j, h] = (rel * (w @ np.abs(vv)) + 2.0 ** -36 * np.abs(vv).sum(0)
                                            + HALF_STEP[out_type] * np.abs(o) * 1.01)
     return out, bound
 
