@@ -30,7 +30,7 @@
 namespace sbd {
 
 constexpr int kStage = 64;           // keys of a stage
-constexpr int kUnits = 1024;         // runs of 16 keys whose pages and exponents are in LDS at once
+constexpr int kUnits = 256;          // runs of 16 keys whose pages and exponents are in LDS at once
 constexpr float kLift = 11.f, kSlack = 4.f;
 
 namespace {
@@ -38,6 +38,16 @@ namespace {
 // Any byte of w an e4m3 NaN (0x7f or 0xff)
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
+// 16 bytes a lane from base + off, or from p, to 1 KB of LDS.
+__device__ __forceinline__ void copy16(const uint8_t* base, uint32_t off, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, %2"
+      :
+      : "s"(lds), "v"(off), "s"(base)
+      : "memory", "m0");
+}
 __device__ __forceinline__ void copy16(const uint8_t* p, uint32_t lds) {
   asm volatile(
       "s_mov_b32 m0, %0\n\t"
@@ -48,8 +58,24 @@ __device__ __forceinline__ void copy16(const uint8_t* p, uint32_t lds) {
       : "memory", "m0");
 }
 
-// A run of 16 keys: its page (-1 where the table names none) and its exponents (K, then V).
+// Largest of the four lanes r, r + 16, r + 32, r + 48, in each of them.
+__device__ __forceinline__ int max_of_groups(int v) {
+  auto p = __builtin_amdgcn_permlane16_swap((unsigned)v, (unsigned)v, false, false);
+  v = max((int)p[0], (int)p[1]);
+  p = __builtin_amdgcn_permlane32_swap((unsigned)v, (unsigned)v, false, false);
+  return max((int)p[0], (int)p[1]);
+}
+__device__ __forceinline__ float max_of_groups(float v) {
+  auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+
+// A run of 16 keys: where its page's codes of this KV head begin (page 0's where the table names
+// none: page is -1 then) and its exponents.
 struct Unit {
+  int64_t at;
   int page;
   int16_t ke, ve;
 };
@@ -83,7 +109,9 @@ __device__ __forceinline__ void load_pages(const PagedAttnArgs& a, const Seq& q,
   const int* table = a.table + (int64_t)q.b * a.max_pages;
   for (int t = threadIdx.x; t < units; t += blockDim.x) {
     const int p = table[min((key0 + 16 * t) >> q.pshift, a.max_pages - 1)];
-    out[t].page = (unsigned)p < (unsigned)a.c.n_pages ? p : -1;
+    const bool known = (unsigned)p < (unsigned)a.c.n_pages;
+    out[t].page = known ? p : -1;
+    out[t].at = ((int64_t)(known ? p : 0) * a.c.n_kv_heads + q.g) * a.c.page_size * a.c.head_dim;
   }
 }
 __device__ __forceinline__ void load_exponents(const PagedAttnArgs& a, const Seq& q, int units, Unit* out) {
@@ -105,21 +133,30 @@ struct Tiles {
   __device__ static int k_at(int key, int c) { return key * DH + ((c ^ ksw(key)) * 16); }
   __device__ static int v_at(int dim, int u) { return kStage * DH + dim * kStage + ((u ^ ((dim >> 1) & 3)) * 16); }
 
-  // Copy i of a stage (units: its four runs; key: its first key) into `lds`.
-  __device__ static void copy(const PagedAttnArgs& a, const Seq& q, const Unit* units, int key, int i, uint32_t lds) {
-    const int lane = threadIdx.x & 63, H = a.c.n_kv_heads, P = a.c.page_size;
-    const uint8_t* p;
-    if (i < kCopies / 2) {
-      const int piece = 64 * i + lane, row = piece / (DH / 16), c = (piece % (DH / 16)) ^ ksw(row);
-      const int u = 64 * i / (DH / 16) / 16;  // the copy's run
-      const int page = max(units[u].page, 0), off = ((key + 16 * u) & (P - 1)) + (row & 15);
-      p = a.c.k_codes + (((int64_t)page * H + q.g) * P + off) * DH + c * 16;
-    } else {
-      const int dim = 16 * (i - kCopies / 2) + (lane >> 2), u = (lane & 3) ^ ((lane >> 3) & 3);
-      const int page = max(units[u].page, 0), off = (key + 16 * u) & (P - 1);
-      p = a.c.v_codes + (((int64_t)page * H + q.g) * DH + dim) * P + off;
+  // Copies w, w + RW, ... of a stage (units: its four runs; key: its first key) into `lds`.
+  // A copy of K lies in one run; of V it holds 16 dimensions of all four.
+  template <int RW>
+  __device__ __forceinline__ static void copy(const PagedAttnArgs& a, const Unit* units, int key, int w, uint32_t lds) {
+    constexpr int kHalf = kCopies / 2, kEach = RW <= kHalf ? kHalf / RW : 1;
+    const int lane = threadIdx.x & 63, P = a.c.page_size;
+    if (RW <= kHalf || w < kHalf) {
+#pragma unroll
+      for (int n = 0; n < kEach; ++n) {
+        const int i = w + RW * n, piece = 64 * i + lane, row = piece / (DH / 16), c = (piece % (DH / 16)) ^ ksw(row);
+        const int run = 64 * i / (DH / 16) / 16;
+        const int64_t at = units[run].at + ((key + 16 * run) & (P - 1)) * DH;
+        const uint64_t base = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)at) |
+                              (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32;
+        copy16(a.c.k_codes + base, (uint32_t)((row & 15) * DH + c * 16), __builtin_amdgcn_readfirstlane(lds + i * 1024));
+      }
     }
-    copy16(p, __builtin_amdgcn_readfirstlane(lds + i * 1024));
+    if (RW <= kHalf || w >= kHalf) {
+      const int u = (lane & 3) ^ ((lane >> 3) & 3), first = RW <= kHalf ? w : w - kHalf;
+      const uint8_t* v = a.c.v_codes + units[u].at + (16 * first + (lane >> 2)) * P + ((key + 16 * u) & (P - 1));
+#pragma unroll
+      for (int n = 0; n < kEach; ++n)
+        copy16(v + 16 * RW * n * P, __builtin_amdgcn_readfirstlane(lds + (kHalf + first + RW * n) * 1024));
+    }
   }
 };
 
@@ -234,14 +271,11 @@ struct Rows {
       float top = -INFINITY;
 #pragma unroll
       for (int u = 0; u < 4; ++u) top = fmaxf(fmaxf(top, fmaxf(s[t][u][0], s[t][u][1])), fmaxf(s[t][u][2], s[t][u][3]));
-      top *= ke;
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
+      top = max_of_groups(top * ke);
       mn[t] = top > m[t] + kSlack || m[t] == -INFINITY ? fmaxf(top, m[t]) : m[t];
       up |= mn[t] != m[t];
     }
-    int vtop = max(max(__shfl(ve, 0), __shfl(ve, 16)), max(__shfl(ve, 32), __shfl(ve, 48)));
-    vtop = __builtin_amdgcn_readfirstlane(max(vtop, -100));
+    const int vtop = __builtin_amdgcn_readfirstlane(max(max_of_groups(ve), -100));
     if (__any(up) || vtop > E) {
       const int e = max(E, vtop);
       const float f = E < -100 ? 0.f : ldexpf(1.f, E - e);
@@ -378,25 +412,22 @@ __device__ __forceinline__ void store_out(const PagedAttnArgs& a, int row, int a
 
 }  // namespace
 
-// A workgroup has RW x KW waves.  RW of them, with 16 RT rows each, share a ring of NB stage
-// buffers; the KW groups hold the same rows and take the stages of a part of the keys in turn, and
-// are joined at the end.  Measured at these shapes (see paged_attention_plan for the choice): a
-// few rows need all waves to bring keys (KW = 4, 64 KB in flight on a CU); with 64 rows and more
-// every wave has rows of its own and nothing is joined; many rows take two tiles a wave and two
-// waves a SIMD, so that the products of one run beside the exponentials and conversions of the
-// other.
-template <class T, int DH, int RT, int RW, int KW, int NB>
-__global__ __launch_bounds__(64 * RW * KW, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedAttnArgs a) {
+// A workgroup has RW waves with 16 RT rows each that share two stage buffers, one barrier a stage:
+// one stage is on its way while the other is used.  What hides the latency of both is the number
+// of workgroups on a CU, so LDS is kept small (36 KB at head_dim 128): with rings of four buffers
+// and half the workgroups 32 sequences x 8 rows x 2312 keys took 79 us instead of 48.  The keys
+// are split over workgroups where the rows do not fill the chip.  Where there are many rows two
+// tiles a wave share the conversion of the codes (3 prompts of 2500 rows: 341 us, one tile 365).
+template <class T, int DH, int RT, int RW>
+__global__ __launch_bounds__(64 * RW, RW == 4 ? 2 : 1) void paged_attn_kernel(PagedAttnArgs a) {
   using L = Tiles<DH>;
-  constexpr int NDT = DH / 16, TR = 16 * RT * RW, kKeys = kStage * KW;  // rows of a workgroup, keys of a round
-  constexpr int kEach = L::kCopies / RW;                              // copies of a wave and stage
-  static_assert(kEach * RW == L::kCopies && NDT % KW == 0, "whole copies, whole tiles to join");
-  constexpr int kRing = KW * NB * L::kBytes, kJoin = KW == 1 ? 0 : KW * RW * RT * NDT * 1024;
-  __shared__ __attribute__((aligned(1024))) uint8_t s_buf[kRing > kJoin ? kRing : kJoin];
+  constexpr int NDT = DH / 16, TR = 16 * RT * RW, NB = 2;
+  constexpr int kEach = L::kCopies / RW;  // copies of a wave and stage
+  static_assert(kEach * RW == L::kCopies, "whole copies");
+  __shared__ __attribute__((aligned(1024))) uint8_t s_buf[NB * L::kBytes];
   __shared__ Unit s_unit[kUnits];
   __shared__ int s_kmax[RW];
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, grp = lane >> 4;
-  const int rw = w % RW, kw = w / RW;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = lane >> 4;
   const int H = a.c.n_kv_heads, G = a.n_q / H;
   const int g = blockIdx.x % H, item = blockIdx.x / H;
   const int split = item % a.plan.n_splits;
@@ -407,8 +438,8 @@ __global__ __launch_bounds__(64 * RW * KW, RT == 1 ? 2 : 1) void paged_attn_kern
   const int64_t rb = rb_all - start(b);
   if (sq.r0 < 0 || sq.n <= 0 || rb < 0 || rb * TR >= (int64_t)sq.n * G) return;
   Rows<T, DH, RT> rows;
-  rows.init(a, sq, rb * TR + 16 * RT * rw);
-  if (lane == 0 && kw == 0) s_kmax[rw] = rows.kmax;
+  rows.init(a, sq, rb * TR + 16 * RT * w);
+  if (lane == 0) s_kmax[w] = rows.kmax;
   __syncthreads();
   int kmax = 0;
 #pragma unroll
@@ -418,131 +449,78 @@ __global__ __launch_bounds__(64 * RW * KW, RT == 1 ? 2 : 1) void paged_attn_kern
   const int k1 = (int)min((int64_t)k0 + len, (int64_t)kmax);
 
   bool flipped = a.scale_log2 >= 0.f;
-  uint8_t* ring = s_buf + kw * NB * L::kBytes;
   for (int seg = k0; seg < k1; seg += 16 * kUnits) {
-    const int end = min(seg + 16 * kUnits, k1), rounds = (end - seg + kKeys - 1) / kKeys;
+    const int end = min(seg + 16 * kUnits, k1), stages = (end - seg + kStage - 1) / kStage;
     if (seg != k0) __syncthreads();
-    load_pages(a, sq, seg, rounds * kKeys / 16, s_unit);
+    load_pages(a, sq, seg, 4 * stages, s_unit);
     __syncthreads();
-    // this group's stage of round i goes to buffer i % NB; behind the last one it is brought again
+    // stage i goes to buffer i % NB; behind the last one it is brought again
     auto copy = [&](int i) {
-      const int at = min(i, rounds - 1) * kKeys + kStage * kw;
-#pragma unroll
-      for (int u = 0; u < kEach; ++u)
-        L::copy(a, sq, s_unit + at / 16, seg + at, u * RW + rw, lds_addr(ring) + i % NB * L::kBytes);
+      const int st = min(i, stages - 1);
+      L::template copy<RW>(a, s_unit + 4 * st, seg + kStage * st, w, lds_addr(s_buf) + i % NB * L::kBytes);
     };
 #pragma unroll
     for (int i = 0; i < NB - 1; ++i) copy(i);
-    load_exponents(a, sq, rounds * kKeys / 16, s_unit);
+    load_exponents(a, sq, 4 * stages, s_unit);
     if (!flipped) rows.flip();
     flipped = true;
-    for (int i = 0; i < rounds; ++i) {
-      vm_wait<(NB - 2) * kEach>();  // this wave's copies of round i have landed
+    for (int i = 0; i < stages; ++i) {
+      vm_wait<(NB - 2) * kEach>();  // this wave's copies of stage i have landed
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      copy(i + NB - 1);  // into the buffer of round i - 1, which every wave has read
-      const int at = i * kKeys + kStage * kw, ks = seg + at;
-      if (ks < rows.kmax && ks < k1) rows.stage(ring + i % NB * L::kBytes, ks, s_unit[at / 16 + grp], fabsf(a.scale_log2));
+      copy(i + NB - 1);  // into the buffer of stage i - 1, which every wave has read
+      const int ks = seg + kStage * i;
+      if (ks < rows.kmax) rows.stage(s_buf + i % NB * L::kBytes, ks, s_unit[4 * i + grp], fabsf(a.scale_log2));
     }
     vm_wait<0>();
   }
 
   const bool last = a.plan.n_splits == 1;
-  auto put = [&](int t, int d, f32x4 x) {
-    const int dim = 16 * d + 4 * grp;
-    if (last)
-      store_out<T>(a, rows.row[t], rows.head[t] * DH + dim, x);
-    else
-      *(f32x4*)(a.part_o + (((int64_t)split * a.rows + rows.row[t]) * a.n_q + rows.head[t]) * DH + dim) = x;
-  };
-  auto put_ml = [&](int t, float m, float l) {
-    if (last || grp != 0 || kw != 0) return;
-    float* ml = a.part_ml + 2 * (((int64_t)split * a.rows + rows.row[t]) * a.n_q + rows.head[t]);
-    ml[0] = m;
-    ml[1] = l;
-  };
-  const bool none = !last && k0 >= k1;  // the join leaves out parts whose sum is 0
-  if constexpr (KW == 1) {
-    const float real = pow2i(max(rows.E, -100));
+  const float real = pow2i(max(rows.E, -100));
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      if (rows.row[t] < 0) continue;
-      const float l = rows.l[t][0], inv = l == 0.f ? 0.f : real / l;
-      put_ml(t, rows.m[t], l);
-      if (none) continue;
-#pragma unroll
-      for (int d = 0; d < NDT; ++d) put(t, d, rows.o[t][d] * inv);
+  for (int t = 0; t < RT; ++t) {
+    if (rows.row[t] < 0) continue;
+    const int64_t part = ((int64_t)split * a.rows + rows.row[t]) * a.n_q + rows.head[t];
+    const float l = rows.l[t][0], inv = l == 0.f ? 0.f : real / l;
+    if (!last && grp == 0) {
+      a.part_ml[2 * part] = rows.m[t];
+      a.part_ml[2 * part + 1] = l;
     }
-  } else {
-    // Every group brings its outputs to the common reference and unit; each adds up its share of
-    // the dimensions.
-    __shared__ float s_m[KW][TR], s_l[KW][TR];
-    __shared__ int s_e[KW][RW];
+    if (!last && k0 >= k1) continue;  // the join leaves out parts whose sum is 0
 #pragma unroll
-    for (int t = 0; t < RT; ++t)
-      if (grp == 0) {
-        s_m[kw][16 * (RT * rw + t) + r] = rows.m[t];
-        s_l[kw][16 * (RT * rw + t) + r] = rows.l[t][0];
-      }
-    if (lane == 0) s_e[kw][rw] = rows.E;
-    __syncthreads();
-    int E = -100;
-#pragma unroll
-    for (int v = 0; v < KW; ++v) E = max(E, s_e[v][rw]);
-    const float unit = rows.E < -100 ? 0.f : ldexpf(1.f, rows.E - E), real = pow2i(E);
-    f32x4* s_o = reinterpret_cast<f32x4*>(s_buf);
-    auto slot = [&](int v, int t, int d) { return (((v * RW + rw) * RT + t) * NDT + d) * 64 + lane; };
-    float lsum[RT], mall[RT];
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      const int i = 16 * (RT * rw + t) + r;
-      float mx = -INFINITY;
-#pragma unroll
-      for (int v = 0; v < KW; ++v) mx = fmaxf(mx, s_m[v][i]);
-      const float base = mx == -INFINITY ? 0.f : mx;
-      lsum[t] = 0.f;
-#pragma unroll
-      for (int v = 0; v < KW; ++v) lsum[t] += s_l[v][i] * __builtin_amdgcn_exp2f(s_m[v][i] - base);
-      mall[t] = mx;
-      const float f = __builtin_amdgcn_exp2f(rows.m[t] - base) * unit;
-#pragma unroll
-      for (int d = 0; d < NDT; ++d) {
-        rows.o[t][d] *= f;
-        if (d / (NDT / KW) != kw) s_o[slot(kw, t, d)] = rows.o[t][d];
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      if (rows.row[t] < 0) continue;
-      const float inv = lsum[t] == 0.f ? 0.f : real / lsum[t];
-      put_ml(t, mall[t], lsum[t]);
-      if (none) continue;
-#pragma unroll
-      for (int d = 0; d < NDT; ++d) {
-        if (d / (NDT / KW) != kw) continue;
-        f32x4 x = rows.o[t][d];
-#pragma unroll
-        for (int v = 0; v < KW; ++v)
-          if (v != kw) x += s_o[slot(v, t, d)];
-        put(t, d, x * inv);
-      }
+    for (int d = 0; d < NDT; ++d) {
+      const f32x4 x = rows.o[t][d] * inv;
+      const int dim = 16 * d + 4 * grp;
+      if (last)
+        store_out<T>(a, rows.row[t], rows.head[t] * DH + dim, x);
+      else
+        *(f32x4*)(a.part_o + part * DH + dim) = x;
     }
   }
 }
 
 // Join the key parts of one (row, query head) pair, each normalised by itself: one wave each, in
 // order of the parts.
-template <class T, int DH>
+template <class T, int DH, int kBatch>
 __global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t pairs = (int64_t)a.rows * a.n_q;
   const int64_t pair = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (pair >= pairs) return;
   const int row = (int)(pair / a.n_q), head = (int)(pair % a.n_q);
-  if (row < a.row_start[0] || row >= a.row_start[a.batch]) return;
+  const bool padding = row < a.row_start[0] || row >= a.row_start[a.batch];
   const int ns = a.plan.n_splits;  // <= 64
+  // Outputs are requested before the sums that tell which parts have some are there.
+  constexpr int PER = DH / 64;
+  typedef float Part __attribute__((ext_vector_type(PER)));
+  Part x[kBatch];
+  auto load = [&](int s0) {
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+      if (s0 + u < ns) x[u] = *(const Part*)(a.part_o + ((s0 + u) * pairs + pair) * DH + PER * lane);
+  };
+  load(0);
   float ms = -INFINITY, ls = 0.f;
   if (lane < ns) {
     ms = a.part_ml[2 * (lane * pairs + pair)];
@@ -551,24 +529,18 @@ __global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a) {
   const float mx = wave_max(ms);
   const float wgt = __builtin_amdgcn_exp2f(ms - (mx == -INFINITY ? 0.f : mx)) * ls;
   const float lsum = wave_sum(wgt);
-  constexpr int PER = DH / 64;
   float acc[PER] = {};
   const uint64_t parts = __ballot(!(ls == 0.f));  // the others have no outputs
-  constexpr int kBatch = 8;
   for (int s0 = 0; s0 < ns; s0 += kBatch) {
-    float x[kBatch][PER];
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u)
-#pragma unroll
-      for (int e = 0; e < PER; ++e)
-        x[u][e] = (parts >> (s0 + u) & 1) ? a.part_o[((s0 + u) * pairs + pair) * DH + PER * lane + e] : 0.f;
+    if (s0 > 0) load(s0);
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-      const float f = __shfl(wgt, (s0 + u) & 63);
+      const float f = __shfl(wgt, s0 + u);
 #pragma unroll
-      for (int e = 0; e < PER; ++e) acc[e] += (parts >> (s0 + u) & 1) ? f * x[u][e] : 0.f;
+      for (int e = 0; e < PER; ++e) acc[e] += (s0 + u < ns && (parts >> (s0 + u) & 1)) ? f * x[u][e] : 0.f;
     }
   }
+  if (padding) return;
   const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
   uint16_t* out = static_cast<uint16_t*>(a.out) + row * a.out_stride + head * DH + PER * lane;
   if constexpr (PER == 2)
@@ -577,20 +549,30 @@ __global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a) {
     *out = (uint16_t)pack2<T>(acc[0] * inv, 0.f);
 }
 
-// The shapes: 0: 16 rows, four key groups; 1: 32 rows, two; 2: 64 rows, one; 3: 256 rows, one.
-static constexpr int kShapeRows[] = {16, 32, 64, 256}, kShapeKeys[] = {256, 128, 64, 64};
+// Workgroups that a call is split into where it has fewer: four a CU.  Half as many leave CUs idle
+// behind ragged lengths (the 32 sequences above: 62 us), twice as many write and read more partial
+// outputs than they save (58 us).
+constexpr int kWant = 1024;
+// The same where a sequence has more than 64 (row, query head) pairs of a KV head: one a CU, and
+// parts of 1024 keys at least (500 rows of a prompt: 16 us in one part, 22 in two; 1000: 28, 45).
+constexpr int kWantMany = 256, kPartMany = 1024;
+// Rows of a workgroup of each shape.  The smallest shape that holds a sequence's rows is taken, so
+// that its keys are read once; the last one from 256 workgroups on (1000 rows of a prompt, 250 of them:
+// 28 us with the third, 37 with the last).
+static constexpr int kShapeRows[] = {16, 32, 64, 128};
 
 PagedAttnPlan paged_attention_plan(const sbd_paged_kv& c, int batch, int rows, int n_q, int max_kv) {
   PagedAttnPlan p{};
   const int64_t pairs = (int64_t)rows * (n_q / c.n_kv_heads);
   const int64_t each = (pairs + batch - 1) / batch;  // of a sequence, on average
-  p.shape = pairs / 256 * c.n_kv_heads >= 128 ? 3 : each <= 16 ? 0 : each <= 32 ? 1 : 2;
-  const int tr = kShapeRows[p.shape], round = kShapeKeys[p.shape];
+  p.shape = pairs / 128 * c.n_kv_heads >= 256 && each > 64 ? 3 : each <= 16 ? 0 : each <= 32 ? 1 : 2;
+  const int tr = kShapeRows[p.shape];
   p.rowblocks = pairs / tr + batch;
   const int64_t groups = std::max<int64_t>(1, batch * ((each + tr - 1) / tr) * c.n_kv_heads);
-  const int64_t want = p.shape == 3 ? 1 : ((p.shape == 0 ? 256 : 512) + groups - 1) / groups;
-  p.n_splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, 64, (max_kv + round - 1) / round}));
-  p.split_keys = ((max_kv + p.n_splits - 1) / p.n_splits + round - 1) / round * round;
+  const bool many = each > 64;
+  const int64_t want = ((many ? kWantMany : kWant) + groups - 1) / groups, part = many ? kPartMany : kStage;
+  p.n_splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, 64, (max_kv + part - 1) / part}));
+  p.split_keys = ((max_kv + p.n_splits - 1) / p.n_splits + kStage - 1) / kStage * kStage;
   if (p.n_splits > 1) {
     const size_t items = (size_t)p.n_splits * rows * n_q;
     p.part_ml = 0;
@@ -608,13 +590,18 @@ static hipError_t launch_dh(const PagedAttnArgs& a, hipStream_t s) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3((unsigned)threads), 0, s, a);
   };
   switch (a.plan.shape) {
-    case 0: go(paged_attn_kernel<T, DH, 1, 1, 4, 2>, 256); break;
-    case 1: go(paged_attn_kernel<T, DH, 1, 2, 2, 2>, 256); break;
-    case 2: go(paged_attn_kernel<T, DH, 1, 4, 1, 4>, 256); break;
-    default: go(paged_attn_kernel<T, DH, 2, 8, 1, 4>, 512); break;
+    case 0: go(paged_attn_kernel<T, DH, 1, 1>, 64); break;
+    case 1: go(paged_attn_kernel<T, DH, 1, 2>, 128); break;
+    case 2: go(paged_attn_kernel<T, DH, 1, 4>, 256); break;
+    default: go(paged_attn_kernel<T, DH, 2, 4>, 256); break;
   }
-  if (a.plan.n_splits > 1)
-    hipLaunchKernelGGL((paged_attn_join_kernel<T, DH>), dim3((unsigned)(((int64_t)a.rows * a.n_q + 3) / 4)), dim3(256), 0, s, a);
+  if (a.plan.n_splits > 1) {
+    const dim3 join((unsigned)(((int64_t)a.rows * a.n_q + 3) / 4));
+    if (a.plan.n_splits <= 4)
+      hipLaunchKernelGGL((paged_attn_join_kernel<T, DH, 4>), join, dim3(256), 0, s, a);
+    else
+      hipLaunchKernelGGL((paged_attn_join_kernel<T, DH, 16>), join, dim3(256), 0, s, a);
+  }
   return hipGetLastError();
 }
 

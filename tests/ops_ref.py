@@ -89,8 +89,9 @@ def append(codes, exps, x, starts, slots, page):
             r += m
 
 
-def attend(q, k_codes, v_codes, k_exp, v_exp, table, starts, kv_len, n_causal, scale, page, out_type):
-    """(out, bound): float64 attention of every row, and how far the kernel may be from it.
+def attend(q, k_codes, v_codes, k_exp, v_exp, table, starts, kv_len, n_causal, scale, page, out_type, only=None):
+    """(out, bound): float64 attention of every row (of `only`, if given), and how far the kernel
+    may be from it.
 
     Bound, from the kernel's arithmetic: the weights are fp16 and held as 2^11 times a power of
     two that is at most the row's largest, so they are off by 2^-11 of themselves or by half of
@@ -113,7 +114,7 @@ def attend(q, k_codes, v_codes, k_exp, v_exp, table, starts, kv_len, n_causal, s
         known = (pages >= 0) & (pages < k_exp.shape[0])
         pages = np.where(known, pages, 0)
         for j in range(n):
-            if starts[b] + j >= rows:
+            if starts[b] + j >= rows or (only is not None and starts[b] + j not in only):
                 continue
             end = L - n + j + 1 if (n_causal is None or j < n_causal[b]) else L
             see = known & (pos < end)
