@@ -133,11 +133,32 @@ __device__ __forceinline__ f32x4 block_product(i32x8 a, i32x8 b) {
 __device__ __forceinline__ i32x8 join8(i32x4 lo, i32x4 hi) {
   return i32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
 }
-// This lane's fragment of block c of a row of k codes (zeros behind its end).
-__device__ __forceinline__ i32x8 load_frag(const uint8_t* row, int c, int grp, int k) {
-  const int k0 = 128 * c + 16 * grp;
-  const i32x4 z{0, 0, 0, 0};
-  return join8(k0 < k ? ld16(row + k0) : z, k0 + 64 < k ? ld16(row + k0 + 64) : z);
+// This lane's fragment of block c of 16 rows of k codes (zeros behind their end), lane group grp
+// holding k = 32 grp .. + 32 here.  The lanes of a pair first read 32 neighbouring bytes of the
+// even row, then of the odd one, and swap halves: a lane that read its own row's pieces would have
+// a neighbour in another row, and the vector cache would be asked for 16 bytes at a time.
+struct RowPair {
+  const uint8_t *even, *odd;  // this lane's pair of rows, its piece of block 0
+};
+__device__ __forceinline__ RowPair row_pair(const uint8_t* base, int64_t stride, int first, int rows) {
+  const int lane = threadIdx.x & 63, r = lane & 15, grp = lane >> 4, piece = 32 * grp + 16 * (r & 1);
+  return RowPair{base + min(first + (r & ~1), rows - 1) * stride + piece, base + min(first + (r | 1), rows - 1) * stride + piece};
+}
+__device__ __forceinline__ i32x8 load_frag(RowPair p, int c, int k) {
+  const int lane = threadIdx.x & 63, k0 = 128 * c + 32 * (lane >> 4) + 16 * (lane & 1);
+  i32x4 a{0, 0, 0, 0}, b = a, lo, hi;
+  if (k0 < k) {
+    a = ld16(p.even + 128 * c);
+    b = ld16(p.odd + 128 * c);
+  }
+  const bool odd = lane & 1;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int sa = __builtin_amdgcn_mov_dpp(a[i], 0xb1, 0xf, 0xf, true), sb = __builtin_amdgcn_mov_dpp(b[i], 0xb1, 0xf, 0xf, true);
+    lo[i] = odd ? sb : a[i];
+    hi[i] = odd ? b[i] : sa;
+  }
+  return join8(lo, hi);
 }
 
 template <class T>
@@ -173,53 +194,44 @@ __device__ __forceinline__ bool vec_ok(const MatmulArgs& a) {
 }
 
 // At most 16 MT rows: the weights' bytes are all there is.  A workgroup makes 16 NT columns of
-// all rows; its eight waves take the blocks of K in turn, kSkinnyDepth of them requested before
-// the first is used, and are joined through LDS.
-constexpr int kSkinnyWaves = 8;
-template <class T, int MT, int NT>
-__global__ __launch_bounds__(64 * kSkinnyWaves, 2) void skinny_kernel(MatmulArgs a) {
+// all rows; its KW waves take the blocks of K in turn and are joined through LDS.  Other waves of
+// the CU hide the latency: two blocks a wave in flight take registers from them and are slower
+// (16 x 114688 x 4096: 94 us, 5.0 TB/s, with one, 107 us with two, 141 us with four).
+template <class T, int MT, int NT, int KW>
+__global__ __launch_bounds__(64 * KW) void skinny_kernel(MatmulArgs a) {
   constexpr bool WIDE = std::is_same_v<T, float>;
-  constexpr int kDepth = MT == 1 ? 4 : 2;
-  __shared__ f32x4 s_acc[kSkinnyWaves][MT * NT][64];
+  __shared__ f32x4 s_acc[KW][MT * NT][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r = lane & 15, grp = lane >> 4;
   const int kb = (a.k + 127) / 128, n0 = blockIdx.x * 16 * NT;
-  const uint8_t* xr[MT];
+  RowPair xr[MT], wr[NT];
   int m[MT];
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
     m[t] = min(16 * t + r, a.m - 1);
-    xr[t] = a.a + m[t] * a.a_stride;
+    xr[t] = row_pair(a.a, a.a_stride, 16 * t, a.m);
   }
-  const uint8_t* wr[NT];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) wr[t] = a.b + (int64_t)min(n0 + 16 * t + r, a.n - 1) * a.k;
+  for (int t = 0; t < NT; ++t) wr[t] = row_pair(a.b, a.k, n0 + 16 * t, a.n);
   const float* sb = a.b_scale + (int64_t)(n0 / 128) * kb;
   f32x4 acc[NT][MT];
 #pragma unroll
   for (int i = 0; i < NT; ++i)
 #pragma unroll
     for (int j = 0; j < MT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int c0 = w; c0 < kb; c0 += kDepth * kSkinnyWaves) {
-    i32x8 wf[kDepth][NT], xf[kDepth][MT];
-    float sc[kDepth][MT];
+  for (int c = w; c < kb; c += KW) {
+    i32x8 wf[NT], xf[MT];
+    float sc[MT];
 #pragma unroll
-    for (int u = 0; u < kDepth; ++u) {
-      const int c = c0 + u * kSkinnyWaves;
-      const bool in = c < kb;  // wave-uniform
+    for (int i = 0; i < NT; ++i) wf[i] = load_frag(wr[i], c, a.k);
 #pragma unroll
-      for (int i = 0; i < NT; ++i) wf[u][i] = in ? load_frag(wr[i], c, grp, a.k) : i32x8{0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll
-      for (int j = 0; j < MT; ++j) {
-        xf[u][j] = in ? load_frag(xr[j], c, grp, a.k) : i32x8{0, 0, 0, 0, 0, 0, 0, 0};
-        sc[u][j] = in ? a.a_scale[(int64_t)c * a.m + m[j]] * sb[c] : 0.f;
-      }
+    for (int j = 0; j < MT; ++j) {
+      xf[j] = load_frag(xr[j], c, a.k);
+      sc[j] = a.a_scale[(int64_t)c * a.m + m[j]] * sb[c];
     }
 #pragma unroll
-    for (int u = 0; u < kDepth; ++u)
+    for (int i = 0; i < NT; ++i)
 #pragma unroll
-      for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int j = 0; j < MT; ++j) acc[i][j] += block_product<WIDE>(wf[u][i], xf[u][j]) * sc[u][j];
+      for (int j = 0; j < MT; ++j) acc[i][j] += block_product<WIDE>(wf[i], xf[j]) * sc[j];
   }
 #pragma unroll
   for (int i = 0; i < NT; ++i)
@@ -227,10 +239,10 @@ __global__ __launch_bounds__(64 * kSkinnyWaves, 2) void skinny_kernel(MatmulArgs
     for (int j = 0; j < MT; ++j) s_acc[w][i * MT + j][lane] = acc[i][j];
   __syncthreads();
   // one wave a 16 x 16 tile, the others' sums added in order
-  for (int t = w; t < MT * NT; t += kSkinnyWaves) {
+  for (int t = w; t < MT * NT; t += KW) {
     f32x4 v = s_acc[0][t][lane];
 #pragma unroll
-    for (int u = 1; u < kSkinnyWaves; ++u) v += s_acc[u][t][lane];
+    for (int u = 1; u < KW; ++u) v += s_acc[u][t][lane];
     const int row = 16 * (t % MT) + r, n = n0 + 16 * (t / MT) + 4 * grp;
     if (row < a.m) store4<T>(a.out, row * a.out_stride + n, a.n - n, vec_ok<T>(a), v);
   }
@@ -515,7 +527,9 @@ __global__ __launch_bounds__(256) void join_splits_kernel(MatmulArgs a, int spli
   store4<T>(a.out, row * a.out_stride + n, left, vec_ok<T>(a), v);
 }
 
-// How a product is cut.
+// How a product is cut.  Fewer tiles than CUs are split along K to two workgroups a CU (203 x 4096 x
+// 14336 in bf16, 128 tiles: 31 us with four parts, 44 with two, 35 with eight); from 256 tiles on the
+// join costs more than it gives (1024 x 4096 x 4096: 29.5 us in one part, 34.5 in two).
 struct MatmulPlan {
   enum { kSkinny, kSmall, kMedium, kLarge } kind;
   int tiles_m, tiles_n, splits, blocks_per_split;
@@ -524,7 +538,8 @@ struct MatmulPlan {
 static MatmulPlan matmul_plan(int m, int n, int k, bool wide) {
   MatmulPlan p{};
   const int kb = (k + 127) / 128;
-  if (m <= 64) {
+  // 32 x 4096 x 4096: 7.0 us with the first kernel, 10.7 with tiles; 32 x 28672 x 4096: 35 and 23.5
+  if (m <= 16 || (m <= 32 && n <= 8192)) {
     p.kind = MatmulPlan::kSkinny;
     p.splits = 1;
     return p;
@@ -545,7 +560,7 @@ static MatmulPlan matmul_plan(int m, int n, int k, bool wide) {
   p.tiles_m = (m + bm - 1) / bm;
   p.tiles_n = (n + bn - 1) / bn;
   const int64_t t = (int64_t)p.tiles_m * p.tiles_n;
-  p.splits = p.kind == MatmulPlan::kLarge ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({512 / t, kb / 4, 16}));
+  p.splits = t >= 256 || p.kind == MatmulPlan::kLarge ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({512 / t, kb / 4, 16}));
   p.blocks_per_split = (kb + p.splits - 1) / p.splits;
   p.splits = (kb + p.blocks_per_split - 1) / p.blocks_per_split;
   return p;
@@ -558,17 +573,16 @@ size_t scaled_matmul_bytes(int m, int n, int k) {
 
 template <class T>
 static hipError_t launch_skinny(const MatmulArgs& a, hipStream_t s) {
-  const int mt = (a.m + 15) / 16;
-  auto go = [&](auto kernel, int nt) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((a.n + 16 * nt - 1) / (16 * nt))), dim3(64 * kSkinnyWaves), 0, s, a);
+  auto go = [&](auto kernel, int nt, int kw) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((a.n + 16 * nt - 1) / (16 * nt))), dim3(64 * kw), 0, s, a);
   };
+  // few columns: narrow tiles and more waves along K, so that more CUs bring weights (16 x 4096 x
+  // 4096: 5.2 us with eight waves, 7.1 with four); many: two tiles a wave halve the reads of the rows
   const bool two = a.n >= 8192;
-  switch (mt) {
-    case 1: two ? go(skinny_kernel<T, 1, 2>, 2) : go(skinny_kernel<T, 1, 1>, 1); break;
-    case 2: two ? go(skinny_kernel<T, 2, 2>, 2) : go(skinny_kernel<T, 2, 1>, 1); break;
-    case 3: two ? go(skinny_kernel<T, 3, 2>, 2) : go(skinny_kernel<T, 3, 1>, 1); break;
-    default: two ? go(skinny_kernel<T, 4, 2>, 2) : go(skinny_kernel<T, 4, 1>, 1); break;
-  }
+  if (a.m <= 16)
+    two ? go(skinny_kernel<T, 1, 2, 4>, 2, 4) : go(skinny_kernel<T, 1, 1, 8>, 1, 8);
+  else
+    two ? go(skinny_kernel<T, 2, 2, 4>, 2, 4) : go(skinny_kernel<T, 2, 1, 8>, 1, 8);
   return hipGetLastError();
 }
 

@@ -28,23 +28,16 @@ from .binding import PagedKVArgs, PageTableArgs, _check, load_library
 TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}  # SBD_TYPE_*
 
 
-class _On:
-    """Makes the tensors' device the current one for a call and gives torch's current stream on it."""
-
-    def __init__(self, device: torch.device):
-        self.device = device
-        self.before = None
-
-    def __enter__(self):
-        index = self.device.index
-        if index is not None and index != torch.cuda.current_device():
-            self.before = torch.cuda.current_device()
-            torch.cuda.set_device(index)
-        return torch.cuda.current_stream().cuda_stream
-
-    def __exit__(self, *exc):
-        if self.before is not None:
-            torch.cuda.set_device(self.before)
+def _run(fn, device: torch.device, where: str, *args):
+    """fn(stream, *args) with the tensors' device as the current one, on torch's current stream of it."""
+    index = device.index
+    if index == torch._C._cuda_getDevice():
+        st = fn(torch._C._cuda_getCurrentRawStream(index), *args)
+    else:
+        with torch.cuda.device(index):
+            st = fn(torch._C._cuda_getCurrentRawStream(index), *args)
+    if st != 0:
+        _check(load_library(), st, where)
 
 
 def _tensor(t, what: str, dtype, shape, device=None):
@@ -147,12 +140,10 @@ class PageTable:
         p_rel = None if release is None else _tensor(release, "release", torch.uint8, (B,), dev)
         if rows < 0:
             raise ValueError(f"rows {rows} is negative")
-        with _On(dev) as stream:
-            buf = torch.empty(rows + 5 * B + 3, dtype=torch.int32, device=dev)
-            step = PagedStep._of_buffer(self.table, self.page_size, rows, buf)
-            _check(self.lib, self.lib.sbd_paged_plan(stream, self._p, p_new, p_rel, rows, step.p_row_start,
-                                                     step.p_kv_len, step.p_slots, step.p_kv_len + 4 * B),
-                   "sbd_paged_plan")
+        buf = torch.empty(rows + 5 * B + 3, dtype=torch.int32, device=dev)
+        step = PagedStep._of_buffer(self.table, self.page_size, rows, buf)
+        _run(self.lib.sbd_paged_plan, dev, "sbd_paged_plan", self._p, p_new, p_rel, rows, step.p_row_start,
+             step.p_kv_len, step.p_slots, step.p_kv_len + 4 * B)
         return step
 
 
@@ -199,10 +190,8 @@ class PagedKV:
         self._step(step, v, "v")
         if k.dtype != v.dtype:
             raise ValueError("k and v have different types")
-        with _On(self.device) as stream:
-            _check(self.lib, self.lib.sbd_paged_append(stream, self._p, TYPES[k.dtype], step.batch, step.rows,
-                                                       step.p_row_start, step.p_slots, pk, sk, pv, sv),
-                   "sbd_paged_append")
+        _run(self.lib.sbd_paged_append, self.device, "sbd_paged_append", self._p, TYPES[k.dtype], step.batch, step.rows,
+             step.p_row_start, step.p_slots, pk, sk, pv, sv)
 
     def attend(self, step: PagedStep, q: torch.Tensor, n_causal: Optional[torch.Tensor] = None,
                scale: Optional[float] = None, max_kv: Optional[int] = None,
@@ -222,21 +211,21 @@ class PagedKV:
         width = step.max_pages * self.page_size
         kv = width if max_kv is None else int(max_kv)
         need = ctypes.c_size_t(0)
-        with _On(self.device) as stream:
-            if out is None:
-                out = torch.empty((step.rows, n_q, self.head_dim), dtype=q.dtype, device=self.device)
+        if out is None:
+            out = torch.empty((step.rows, n_q, self.head_dim), dtype=q.dtype, device=self.device)
+            po, so = out.data_ptr(), n_q * self.head_dim
+        else:
             po, so = _rows(out, "out", n_q, self.head_dim, self.device)
             self._step(step, out, "out")
             if out.dtype != q.dtype:
                 raise ValueError("out has another type than q")
-            _check(self.lib, self.lib.sbd_paged_attention_workspace(self._p, step.batch, step.rows, n_q, kv,
-                                                                    ctypes.byref(need)),
-                   "sbd_paged_attention_workspace")
-            ws = torch.empty(need.value, dtype=torch.uint8, device=self.device) if need.value else None
-            _check(self.lib, self.lib.sbd_paged_attention(
-                stream, self._p, TYPES[q.dtype], step.batch, step.rows, n_q, step.p_row_start, step.p_kv_len,
-                step.p_table, step.max_pages, p_nc, 1.0 / math.sqrt(self.head_dim) if scale is None else float(scale),
-                kv, pq, sq, po, so, None if ws is None else ws.data_ptr(), need.value), "sbd_paged_attention")
+        _check(self.lib, self.lib.sbd_paged_attention_workspace(self._p, step.batch, step.rows, n_q, kv,
+                                                                ctypes.byref(need)), "sbd_paged_attention_workspace")
+        ws = torch.empty(need.value, dtype=torch.uint8, device=self.device) if need.value else None
+        _run(self.lib.sbd_paged_attention, self.device, "sbd_paged_attention", self._p, TYPES[q.dtype], step.batch,
+             step.rows, n_q, step.p_row_start, step.p_kv_len, step.p_table, step.max_pages, p_nc,
+             1.0 / math.sqrt(self.head_dim) if scale is None else float(scale), kv, pq, sq, po, so,
+             None if ws is None else ws.data_ptr(), need.value)
         return out
 
 
@@ -251,13 +240,11 @@ def scaled_quantize(x: torch.Tensor, block_rows: int = 1):
         raise ValueError("x: the elements of a row must be contiguous")
     lib = load_library()
     kb = -(-cols // 128)
-    with _On(x.device) as stream:
-        codes = torch.empty((rows, cols), dtype=torch.uint8, device=x.device)
-        shape = (kb, rows) if block_rows == 1 else (-(-rows // 128), kb)
-        scales = torch.empty(shape, dtype=torch.float32, device=x.device)
-        _check(lib, lib.sbd_scaled_quantize(stream, TYPES[x.dtype], rows, cols, x.data_ptr(),
-                                            x.stride(0) if rows > 1 else cols, int(block_rows), codes.data_ptr(),
-                                            scales.data_ptr()), "sbd_scaled_quantize")
+    codes = torch.empty((rows, cols), dtype=torch.uint8, device=x.device)
+    shape = (kb, rows) if block_rows == 1 else (-(-rows // 128), kb)
+    scales = torch.empty(shape, dtype=torch.float32, device=x.device)
+    _run(lib.sbd_scaled_quantize, x.device, "sbd_scaled_quantize", TYPES[x.dtype], rows, cols, x.data_ptr(),
+         x.stride(0) if rows > 1 else cols, int(block_rows), codes.data_ptr(), scales.data_ptr())
     return codes, scales
 
 
@@ -278,17 +265,16 @@ def scaled_matmul(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_sca
     p_as = _tensor(a_scale, "a_scale", torch.float32, (kb, m), dev)
     lib = load_library()
     need = ctypes.c_size_t(0)
-    with _On(dev) as stream:
-        if out is None:
-            if out_dtype not in TYPES:
-                raise ValueError(f"out_dtype {out_dtype}: expected bfloat16, float16 or float32")
-            out = torch.empty((m, n), dtype=out_dtype, device=dev)
-        elif not out.is_cuda or out.device != dev or out.dtype not in TYPES or tuple(out.shape) != (m, n) or (
-                m and n > 1 and out.stride(1) != 1):
-            raise ValueError(f"out: expected a CUDA matrix of shape {(m, n)} with contiguous rows on {dev}")
-        _check(lib, lib.sbd_scaled_matmul_workspace(m, n, k, ctypes.byref(need)), "sbd_scaled_matmul_workspace")
-        ws = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
-        _check(lib, lib.sbd_scaled_matmul(stream, m, n, k, a.data_ptr(), a.stride(0) if m > 1 else k, p_as, p_b, p_bs,
-                                          TYPES[out.dtype], out.data_ptr(), out.stride(0) if m > 1 else n,
-                                          None if ws is None else ws.data_ptr(), need.value), "sbd_scaled_matmul")
+    if out is None:
+        if out_dtype not in TYPES:
+            raise ValueError(f"out_dtype {out_dtype}: expected bfloat16, float16 or float32")
+        out = torch.empty((m, n), dtype=out_dtype, device=dev)
+    elif not out.is_cuda or out.device != dev or out.dtype not in TYPES or tuple(out.shape) != (m, n) or (
+            m and n > 1 and out.stride(1) != 1):
+        raise ValueError(f"out: expected a CUDA matrix of shape {(m, n)} with contiguous rows on {dev}")
+    _check(lib, lib.sbd_scaled_matmul_workspace(m, n, k, ctypes.byref(need)), "sbd_scaled_matmul_workspace")
+    ws = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
+    _run(lib.sbd_scaled_matmul, dev, "sbd_scaled_matmul", m, n, k, a.data_ptr(), a.stride(0) if m > 1 else k, p_as, p_b,
+         p_bs, TYPES[out.dtype], out.data_ptr(), out.stride(0) if m > 1 else n, None if ws is None else ws.data_ptr(),
+         need.value)
     return out
