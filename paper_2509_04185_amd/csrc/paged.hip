@@ -15,51 +15,74 @@ namespace sbd {
 // written (phase 3), each by as many threads as there are items.  A row's slot is formed from
 // the free list itself, not from the table entry another thread writes.
 //
-// scratch: [0, B) index of the first new page relative to base; [B, 2B) pages held before
-// taking; [2B, 3B] scan of the pages given back; [3B + 1] free pages before the call.
+// A step of few items is one launch of one workgroup, which keeps what the scans found in LDS (a
+// chain of loads is all its time); larger ones take a launch for each phase.
 
 constexpr int kPlanThreads = 1024;
+constexpr int kPlanItems = 16 * kPlanThreads;  // table entries or rows that one workgroup takes
 
-// Exclusive scan over the workgroup; total gets the sum.
-__device__ int64_t block_scan(int64_t v, int64_t* waves, int64_t& total) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  int64_t s = v;
+// What phase 1 leaves for the others, per sequence, in scratch or in LDS.
+struct PlanView {
+  int *take;    // [B] first new page, relative to base
+  int *before;  // [B] pages held before taking
+  int *back;    // [B + 1] scan of the pages given back, their number
+  int *free0;   // free pages before the call
+  int *row, *kv, *now, *cached;  // row_start, kv_len, held, cached
+  int *base;                     // free pages afterwards
+};
+
+// Exclusive scans of two values over the workgroup, whose first n threads have some; totals in t.
+__device__ void block_scan2(int64_t (&v)[2], int64_t (&t)[2], int n, int64_t (*waves)[2]) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nw = (min(n, kPlanThreads) + 63) / 64;
+  int64_t s[2] = {v[0], v[1]};
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t u = __shfl_up(s, o);
-    if (lane >= o) s += u;
-  }
+  for (int o = 1; o < 64; o <<= 1)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t u = __shfl_up(s[i], o);
+      if (lane >= o) s[i] += u;
+    }
   __syncthreads();  // waves[] may still be read from the scan before
-  if (lane == 63) waves[w] = s;
-  __syncthreads();
-  int64_t before = 0, all = 0;
-#pragma unroll 1
-  for (int i = 0; i < kPlanThreads / 64; ++i) {
-    if (i < w) before += waves[i];
-    all += waves[i];
+  if (lane == 63) {
+    waves[w][0] = s[0];
+    waves[w][1] = s[1];
   }
-  total = all;
-  return before + s - v;
+  __syncthreads();
+  int64_t before[2] = {0, 0};
+  t[0] = t[1] = 0;
+#pragma unroll 1
+  for (int i = 0; i < nw; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if (i < w) before[j] += waves[i][j];
+      t[j] += waves[i][j];
+    }
+#pragma unroll
+  for (int j = 0; j < 2; ++j) v[j] = before[j] + s[j] - v[j];
 }
 
-__device__ void plan_scans(const PlanArgs& a) {
-  __shared__ int64_t waves[kPlanThreads / 64];
+template <bool LDS>
+__device__ void plan_scans(const PlanArgs& a, const PlanView& o) {
+  __shared__ int64_t waves[kPlanThreads / 64][2];
+  __shared__ int64_t s_taken;
   const sbd_page_table& t = a.t;
   const int B = t.batch, W = t.max_pages;
   const int free0 = min(max(*t.free_count, 0), t.n_pages);
-  int64_t back = 0, total;
+  int64_t back = 0, v[2], total[2];
   if (a.release) {
     for (int b0 = 0; b0 < B; b0 += kPlanThreads) {
       const int b = b0 + threadIdx.x;
-      const int v = (b < B && a.release[b]) ? min(max(t.held[b], 0), W) : 0;
-      const int64_t at = back + block_scan(v, waves, total);
-      if (b < B) a.scratch[2 * B + b] = (int)min(at, (int64_t)t.n_pages);
-      back += total;
+      v[0] = (b < B && a.release[b]) ? min(max(t.held[b], 0), W) : 0;
+      v[1] = 0;
+      block_scan2(v, total, B - b0, waves);
+      if (b < B) o.back[b] = (int)min(back + v[0], (int64_t)t.n_pages);
+      back += total[0];
     }
   }
   const int given = (int)min(back, (int64_t)(t.n_pages - free0));
   const int avail = free0 + given;
-  int64_t need_sum = 0, row_sum = 0, taken = 0;
+  if (threadIdx.x == 0) s_taken = 0;
+  int64_t sums[2] = {0, 0};
   for (int b0 = 0; b0 < B; b0 += kPlanThreads) {
     const int b = b0 + threadIdx.x;
     const bool in = b < B;
@@ -70,72 +93,86 @@ __device__ void plan_scans(const PlanArgs& a) {
     const int64_t tokens = (int64_t)cached + n;
     const bool fits = in && cached >= 0 && n >= 0 && tokens <= (int64_t)W * t.page_size;
     const int need = fits ? max((int)((tokens + t.page_size - 1) / t.page_size) - held, 0) : 0;
-    const int64_t at = need_sum + block_scan(need, waves, total);
-    need_sum += total;
+    v[0] = need;
+    v[1] = max(n, 0);
+    block_scan2(v, total, B - b0, waves);  // its barriers: s_taken is 0 now
+    const int64_t at = sums[0] + v[0], row = sums[1] + v[1];
+    sums[0] += total[0];
+    sums[1] += total[1];
     const bool ok = fits && (need == 0 || at + need <= avail);
-    const int got = ok ? need : 0;
-    block_scan(got, waves, total);
-    taken += total;
-    const int64_t row = row_sum + block_scan(max(n, 0), waves, total);
-    row_sum += total;
+    // those served that need pages come first, so the last of them ends where all that is taken does
+    if (ok && need > 0) atomicMax((unsigned long long*)&s_taken, (unsigned long long)(at + need));
     if (in) {
-      a.scratch[b] = (int)min(at, (int64_t)t.n_pages);
-      a.scratch[B + b] = held;
-      a.row_start[b] = (int)min(row, (int64_t)INT32_MAX);
-      a.kv_len[b] = ok ? (int)tokens : 0;
-      t.held[b] = held + got;
+      o.take[b] = (int)min(at, (int64_t)t.n_pages);
+      o.before[b] = held;
+      const int rs = (int)min(row, (int64_t)INT32_MAX), kv = ok ? (int)tokens : 0, now = held + (ok ? need : 0);
+      a.row_start[b] = rs;
+      a.kv_len[b] = kv;
+      t.held[b] = now;
       if (gone) t.cached[b] = 0;
+      if (LDS) {
+        o.row[b] = rs;
+        o.kv[b] = kv;
+        o.now[b] = now;
+        o.cached[b] = cached;
+      }
     }
   }
+  __syncthreads();
   if (threadIdx.x == 0) {
-    a.row_start[B] = (int)min(row_sum, (int64_t)INT32_MAX);
-    a.scratch[3 * B] = given;
-    a.scratch[3 * B + 1] = free0;
-    *t.free_count = avail - (int)taken;
+    const int rows = (int)min(sums[1], (int64_t)INT32_MAX);
+    a.row_start[B] = rows;
+    o.back[B] = given;
+    *o.free0 = free0;
+    const int left = avail - (int)s_taken;
+    *t.free_count = left;
+    if (LDS) {
+      o.row[B] = rows;
+      *o.base = left;
+    }
   }
 }
 
-__device__ void plan_give_back(const PlanArgs& a, int64_t first, int64_t step) {
+__device__ void plan_give_back(const PlanArgs& a, const PlanView& o, int64_t first, int64_t step) {
   const sbd_page_table& t = a.t;
-  const int B = t.batch, n = a.scratch[3 * B], free0 = a.scratch[3 * B + 1];
-  const int* start = a.scratch + 2 * B;
+  const int B = t.batch, n = o.back[B], free0 = *o.free0;
   for (int64_t i = first; i < n; i += step) {
     int lo = 0, hi = B;  // last sequence that starts at or before i (empty ones before it start there too)
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
-      if (start[mid] <= i) lo = mid; else hi = mid;
+      if (o.back[mid] <= i) lo = mid; else hi = mid;
     }
-    t.free_list[free0 + i] = t.table[(int64_t)lo * t.max_pages + min((int)i - start[lo], t.max_pages - 1)];
+    t.free_list[free0 + i] = t.table[(int64_t)lo * t.max_pages + min((int)i - o.back[lo], t.max_pages - 1)];
   }
 }
 
-__device__ void plan_tables(const PlanArgs& a, int64_t first, int64_t step) {
+__device__ void plan_tables(const PlanArgs& a, const PlanView& o, int64_t first, int64_t step) {
   const sbd_page_table& t = a.t;
-  const int B = t.batch, W = t.max_pages, base = *t.free_count;
+  const int B = t.batch, W = t.max_pages, base = *o.base;
   auto free_page = [&](int b, int col, int held) {
-    return t.free_list[min(max(base + a.scratch[b] + col - held, 0), t.n_pages - 1)];
+    return t.free_list[min(max(base + o.take[b] + col - held, 0), t.n_pages - 1)];
   };
   for (int64_t i = first; i < (int64_t)B * W; i += step) {
-    const int b = (int)(i / W), col = (int)(i % W);
-    const int held = a.scratch[B + b], now = t.held[b];
+    const int b = (int)((uint64_t)i / (unsigned)W), col = (int)(i - (int64_t)b * W);
+    const int held = o.before[b], now = o.now[b];
     if (col >= held && col < now)
       t.table[i] = free_page(b, col, held);
     else if (col >= now && a.release && a.release[b])
       t.table[i] = -1;
   }
-  const int rows = a.row_start[B];
+  const int rows = o.row[B], pshift = 31 - __builtin_clz(t.page_size);
   for (int64_t r = first; r < a.rows; r += step) {
     int slot = -1;
     if (r < rows) {
       int lo = 0, hi = B;  // last sequence that starts at or before r: it is not an empty one
       while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
-        if (a.row_start[mid] <= r) lo = mid; else hi = mid;
+        if (o.row[mid] <= r) lo = mid; else hi = mid;
       }
-      if (a.kv_len[lo] > 0) {
-        const int p = t.cached[lo] + (int)r - a.row_start[lo], col = p / t.page_size, held = a.scratch[B + lo];
+      if (o.kv[lo] > 0) {
+        const int p = o.cached[lo] + (int)r - o.row[lo], col = p >> pshift, held = o.before[lo];
         const int page = col < held ? t.table[(int64_t)lo * W + col] : free_page(lo, col, held);
-        if (page >= 0 && page < t.n_pages) slot = page * t.page_size + p % t.page_size;
+        if (page >= 0 && page < t.n_pages) slot = (page << pshift) + (p & (t.page_size - 1));
       }
     }
     a.slots[r] = slot;
@@ -143,25 +180,34 @@ __device__ void plan_tables(const PlanArgs& a, int64_t first, int64_t step) {
 }
 
 __global__ __launch_bounds__(kPlanThreads) void plan_all_kernel(PlanArgs a) {
-  plan_scans(a);
+  __shared__ int s[7 * kPlanThreads + 4];  // at most kPlanThreads sequences
+  constexpr int N = kPlanThreads;
+  const PlanView o{s, s + N, s + 2 * N, s + 7 * N + 2, s + 3 * N + 1, s + 4 * N + 2, s + 5 * N + 2, s + 6 * N + 2, s + 7 * N + 3};
+  plan_scans<true>(a, o);
   __syncthreads();
   if (a.release) {
-    plan_give_back(a, threadIdx.x, kPlanThreads);
+    plan_give_back(a, o, threadIdx.x, kPlanThreads);
     __syncthreads();
   }
-  plan_tables(a, threadIdx.x, kPlanThreads);
+  plan_tables(a, o, threadIdx.x, kPlanThreads);
 }
-__global__ __launch_bounds__(kPlanThreads) void plan_scans_kernel(PlanArgs a) { plan_scans(a); }
+
+__device__ PlanView scratch_view(const PlanArgs& a) {
+  const int B = a.t.batch;
+  return PlanView{a.scratch, a.scratch + B, a.scratch + 2 * B, a.scratch + 3 * B + 1,
+                  a.row_start, a.kv_len, a.t.held, a.t.cached, a.t.free_count};
+}
+__global__ __launch_bounds__(kPlanThreads) void plan_scans_kernel(PlanArgs a) { plan_scans<false>(a, scratch_view(a)); }
 __global__ __launch_bounds__(256) void plan_give_back_kernel(PlanArgs a) {
-  plan_give_back(a, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
+  plan_give_back(a, scratch_view(a), (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
 }
 __global__ __launch_bounds__(256) void plan_tables_kernel(PlanArgs a) {
-  plan_tables(a, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
+  plan_tables(a, scratch_view(a), (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
 }
 
 hipError_t launch_paged_plan(const PlanArgs& a, hipStream_t s) {
   const int64_t items = std::max<int64_t>((int64_t)a.t.batch * a.t.max_pages, a.rows);
-  if (items <= 16 * kPlanThreads) {
+  if (items <= kPlanItems && a.t.batch <= kPlanThreads) {
     hipLaunchKernelGGL(plan_all_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
     return hipGetLastError();
   }
@@ -223,15 +269,26 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a) {
 
   const int64_t stride = values ? a.v_stride : a.k_stride;
   const uint16_t* x = static_cast<const uint16_t*>(values ? a.v : a.k) + (int64_t)(r0 + j) * stride + (int64_t)head * DH;
+  // A thread's first kHold pieces of 8 elements (all of them up to 64 rows of 128) stay in
+  // registers between the exponent and the codes.
+  constexpr int kHold = 4;
+  i32x4 hold[kHold];
   float amax = 0.f;
-  for (int i = tid; i < m * kPieces; i += kAppendThreads) {
-    const i32x4 w = ld16(x + (int64_t)(i / kPieces) * stride + (i % kPieces) * 8);
+  auto piece = [&](int i) { return ld16(x + (int64_t)(i / kPieces) * stride + (i % kPieces) * 8); };
+  auto largest = [&](i32x4 w) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const f32x2 f = unpack2<T>((uint32_t)w[u]);
       amax = fmaxf(amax, fmaxf(finite_abs(f[0]), finite_abs(f[1])));
     }
-  }
+  };
+#pragma unroll
+  for (int h = 0; h < kHold; ++h)
+    if (tid + h * kAppendThreads < m * kPieces) hold[h] = piece(tid + h * kAppendThreads);
+#pragma unroll
+  for (int h = 0; h < kHold; ++h)
+    if (tid + h * kAppendThreads < m * kPieces) largest(hold[h]);
+  for (int i = tid + kHold * kAppendThreads; i < m * kPieces; i += kAppendThreads) largest(piece(i));
   int8_t* exp = (values ? a.c.v_exp : a.c.k_exp) + (int64_t)page * H + head;
   const int old = *exp;
   int e = block_exponent(block_max(amax));  // its barrier: every thread has read the old exponent
@@ -248,9 +305,8 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a) {
       w[1] = (int)rescale4((uint32_t)w[1], again);
       *(i32x2*)(codes + 8 * i) = w;
     }
-  for (int i = tid; i < m * kPieces; i += kAppendThreads) {
+  auto encode = [&](int i, i32x4 w) {
     const int row = i / kPieces, c = (i % kPieces) * 8;
-    const i32x4 w = ld16(x + (int64_t)row * stride + c);
     float f[8];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
@@ -265,23 +321,45 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a) {
     } else {
       *(i32x2*)(codes + (int64_t)(off + row) * DH + c) = i32x2{(int)lo, (int)hi};
     }
-  }
+  };
+#pragma unroll
+  for (int h = 0; h < kHold; ++h)
+    if (tid + h * kAppendThreads < m * kPieces) encode(tid + h * kAppendThreads, hold[h]);
+  for (int i = tid + kHold * kAppendThreads; i < m * kPieces; i += kAppendThreads) encode(i, piece(i));
   if (!values) return;
   __syncthreads();
-  // 16 tokens of one dimension at a time; a piece that also holds kept or later codes is read first
-  const int first = grown ? 0 : off / 16, last = (off + m + 15) / 16;
-  const int pieces = last - first;
-  for (int i = tid; i < pieces * DH; i += kAppendThreads) {
-    const int d = i / pieces, t0 = (first + i % pieces) * 16;
-    uint8_t* at = codes + (int64_t)d * P + t0;
-    uint32_t w[4] = {0, 0, 0, 0};
-    if (t0 < off || t0 + 16 > off + m) {
-      const i32x4 v = ld16(at);
-#pragma unroll
-      for (int u = 0; u < 4; ++u) w[u] = (uint32_t)v[u];
-    }
+  // Pieces of 16 tokens that are all new: four dimensions at a time, turned around in registers.
+  const int new0 = (off + 15) / 16, new1 = max(new0, (off + m) / 16), whole = new1 - new0;
+  for (int i = tid; i < whole * (DH / 4); i += kAppendThreads) {
+    const int d = i / whole * 4, t0 = (new0 + i % whole) * 16;
+    const uint8_t* from = tile + (t0 - off) * kLd + d;
+    i32x4 out[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
+      uint32_t r[4];
+#pragma unroll
+      for (int v = 0; v < 4; ++v) r[v] = *(const uint32_t*)(from + (4 * u + v) * kLd);
+      const uint32_t lo0 = __builtin_amdgcn_perm(r[1], r[0], 0x05010400), hi0 = __builtin_amdgcn_perm(r[1], r[0], 0x07030602);
+      const uint32_t lo1 = __builtin_amdgcn_perm(r[3], r[2], 0x05010400), hi1 = __builtin_amdgcn_perm(r[3], r[2], 0x07030602);
+      out[0][u] = (int)__builtin_amdgcn_perm(lo1, lo0, 0x05040100);
+      out[1][u] = (int)__builtin_amdgcn_perm(lo1, lo0, 0x07060302);
+      out[2][u] = (int)__builtin_amdgcn_perm(hi1, hi0, 0x05040100);
+      out[3][u] = (int)__builtin_amdgcn_perm(hi1, hi0, 0x07060302);
+    }
+#pragma unroll
+    for (int v = 0; v < 4; ++v) *(i32x4*)(codes + (int64_t)(d + v) * P + t0) = out[v];
+  }
+  // The others also hold kept or later codes (kept ones are all visited where their scale grew):
+  // one dimension at a time, read first.
+  const int first = grown ? 0 : off / 16, last = (off + m + 15) / 16, rest = last - first - whole;
+  for (int i = tid; i < rest * DH; i += kAppendThreads) {
+    const int d = i / rest, q = first + i % rest, t0 = (q < new0 ? q : q + whole) * 16;
+    uint8_t* at = codes + (int64_t)d * P + t0;
+    const i32x4 old = ld16(at);
+    uint32_t w[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      w[u] = (uint32_t)old[u];
       if (grown && t0 + 4 * u < off) {
         const uint32_t r = rescale4(w[u], again);
         const int keep = min(off - t0 - 4 * u, 4);
