@@ -512,7 +512,7 @@ sbd_status sbd_paged_append(void* stream, const sbd_paged_kv* c, int32_t dtype, 
  *              every row is causal.
  *   scale      of the products q.k, finite
  *   max_kv     what the longest kv_len is about, in [1, max_pages * page_size]: it decides
- *              how the keys are split over the chip, not the result beyond summation order
+ *              into how many parts keys are split at most, not the result beyond summation order
  * out = sum_i softmax_i(scale * q.k_i) v_i over the keys a row sees; a row that sees no key
  * (its sequence was not served) gets zeros.  Sums and softmax statistics are fp32; a key
  * whose weight is below 2^-36 of the row's largest may count as zero.  Values of keys that a
@@ -535,7 +535,7 @@ sbd_status sbd_paged_attention(void* stream, const sbd_paged_kv* c, int32_t dtyp
  * [-100, 100] with |x| <= 448 * 2^e for every finite x of the block; code = the e4m3 value
  * nearest to x / scale (ties to even, saturating, NaN stays NaN).
  *   x       SBD_TYPE_* [rows][cols], rows x_stride elements apart; cols a multiple of 16, rows
- *           16-byte aligned
+ *           16-byte aligned, rows * cols at most 2^36
  *   codes   [rows][cols], contiguous, 16-byte aligned
  *   scales  float, block_rows 1: [ceil(cols / 128)][rows] (the scales of one block of columns
  *           lie together); block_rows 128: [ceil(rows / 128)][ceil(cols / 128)]

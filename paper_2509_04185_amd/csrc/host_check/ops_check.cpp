@@ -113,7 +113,9 @@ int main() {
     REFUSES(SBD_ERR_INVALID_ARG, sbd_scaled_matmul(nullptr, 1, bad, 128, u, 128, f, u, f, 0, u, 128, nullptr, 0));
     REFUSES(SBD_ERR_INVALID_ARG, sbd_scaled_matmul(nullptr, 1, 128, bad, u, 128, f, u, f, 0, u, 128, nullptr, 0));
   }
-  RUNS(sbd_scaled_quantize(nullptr, SBD_TYPE_FP32, 1 << 24, 1 << 24, u, (int64_t)1 << 50, 128, u, f));
+  RUNS(sbd_scaled_quantize(nullptr, SBD_TYPE_FP32, 1 << 24, 1 << 12, u, (int64_t)1 << 50, 128, u, f));
+  RUNS(sbd_scaled_quantize(nullptr, SBD_TYPE_FP32, 1 << 12, 1 << 24, u, (int64_t)1 << 50, 1, u, f));
+  REFUSES(SBD_ERR_INVALID_ARG, sbd_scaled_quantize(nullptr, SBD_TYPE_FP32, 1 << 24, 1 << 13, u, 1 << 13, 1, u, f));
   RUNS(sbd_scaled_matmul(nullptr, 1 << 24, 1 << 12, 1 << 22, u, 1 << 22, f, u, f, SBD_TYPE_FP32, u, 1 << 24, nullptr, 0));
   REFUSES(SBD_ERR_INVALID_ARG, sbd_scaled_matmul(nullptr, 1 << 24, 1 << 24, 128, u, 128, f, u, f, 0, u, 1 << 24, nullptr, 0));
   RUNS(sbd_scaled_matmul(nullptr, 7, 1, 16, u, 16, f, u, f, SBD_TYPE_BF16, u + 2, 1, u, 256));

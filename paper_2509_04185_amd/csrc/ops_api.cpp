@@ -146,7 +146,8 @@ sbd_status sbd_paged_attention(void* stream, const sbd_paged_kv* c, int32_t dtyp
   if (max_kv > (int64_t)max_pages * c->page_size)
     return op_fail(SBD_ERR_INVALID_ARG, "max_kv %d exceeds the table's %lld tokens", max_kv,
                    (long long)max_pages * c->page_size);
-  if (!std::isfinite(scale)) return op_fail(SBD_ERR_INVALID_ARG, "scale must be finite");
+  const float scale_log2 = scale * 1.44269504088896340736f;
+  if (!std::isfinite(scale_log2)) return op_fail(SBD_ERR_INVALID_ARG, "scale must be finite (and below 2.3e38 in size)");
   if (rows == 0) return SBD_OK;
   const int64_t width = (int64_t)n_q_heads * c->head_dim;
   if (sbd_status st = check_rows16("q", q, q_stride, width)) return st;
@@ -159,7 +160,7 @@ sbd_status sbd_paged_attention(void* stream, const sbd_paged_kv* c, int32_t dtyp
     return op_fail(SBD_ERR_OUT_OF_MEMORY, "workspace of %zu bytes, need %zu", workspace_bytes, a.plan.bytes);
   a.c = *c; a.batch = batch; a.rows = rows; a.n_q = n_q_heads; a.max_pages = max_pages;
   a.row_start = row_start; a.kv_len = kv_len; a.table = table; a.n_causal = n_causal;
-  a.scale_log2 = scale * 1.44269504088896340736f;
+  a.scale_log2 = scale_log2;
   a.q = q; a.out = out; a.q_stride = q_stride; a.out_stride = out_stride;
   if (a.plan.bytes > 0) {
     a.part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + a.plan.part_ml);
@@ -175,6 +176,7 @@ sbd_status sbd_scaled_quantize(void* stream, int32_t dtype, int32_t rows, int32_
   if (rows < 0 || rows > kMaxOpRows) return op_fail(SBD_ERR_INVALID_ARG, "rows %d out of [0, %d]", rows, kMaxOpRows);
   if (cols < 16 || cols % 16 || cols > kMaxOpRows)
     return op_fail(SBD_ERR_INVALID_ARG, "cols %d is no multiple of 16 in [16, %d]", cols, kMaxOpRows);
+  if ((int64_t)rows * cols > ((int64_t)1 << 36)) return op_fail(SBD_ERR_INVALID_ARG, "rows * cols exceeds 2^36");
   if (block_rows != 1 && block_rows != 128) return op_fail(SBD_ERR_INVALID_ARG, "block_rows must be 1 or 128 (got %d)", block_rows);
   if (rows == 0) return SBD_OK;
   if (!x || !codes || !scales) return op_fail(SBD_ERR_INVALID_ARG, "null argument");

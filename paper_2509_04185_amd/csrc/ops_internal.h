@@ -33,9 +33,9 @@ struct AppendArgs {
 hipError_t launch_paged_append(const AppendArgs& a, int dtype, hipStream_t s);
 
 // How an attention call is cut: the shape of a workgroup (rows are (row, query head) pairs of a
-// KV head), and the keys in n_splits parts of at least split_keys.
+// KV head), and every sequence's keys in n_splits parts.
 struct PagedAttnPlan {
-  int32_t shape, n_splits, split_keys;
+  int32_t shape, n_splits;
   int64_t rowblocks;  // workgroups of one KV head and key part, upper bound
   size_t part_ml, part_o, bytes;  // workspace: (max, sum) and outputs of the key parts
 };

@@ -125,7 +125,7 @@ def test_quantize_refusals(lib):
     def call(dtype=0, rows=4, cols=256, x=A, stride=256, br=1, codes=A, scales=A):
         return lib.sbd_scaled_quantize(None, dtype, rows, cols, x, stride, br, codes, scales)
     for kw, text in ((dict(dtype=3), "type"), (dict(dtype=-1), "type"), (dict(rows=-1), "rows"), (dict(cols=0), "cols"),
-                     (dict(cols=100), "cols"), (dict(cols=8), "cols"), (dict(br=0), "block_rows"), (dict(br=64), "block_rows"),
+                     (dict(cols=100), "cols"), (dict(cols=8), "cols"), (dict(rows=2 ** 20, cols=2 ** 17, stride=2 ** 17), "2^36"), (dict(br=0), "block_rows"), (dict(br=64), "block_rows"),
                      (dict(x=None), "null"), (dict(codes=None), "null"), (dict(scales=None), "null"), (dict(x=A + 2), "aligned"),
                      (dict(codes=A + 8), "aligned"), (dict(stride=240), "stride"), (dict(stride=260), "stride"),
                      (dict(dtype=2, stride=258), "stride")):
