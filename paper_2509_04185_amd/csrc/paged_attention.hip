@@ -82,10 +82,11 @@ struct Unit {
 
 // Keys of a part: every sequence is split evenly, whatever lengths the call expected (parts of one
 // length for all, as long as the longest sequence needs: 32 sequences of 512 to 4104 keys 62 us
-// instead of 53, and twice that where the call did not know how long they are).
+// instead of 53, and twice that where the call did not know how long they are).  Two stages at
+// least: 4 sequences x 16 rows x 2016 keys take 28 us in 32 parts, 21 in 16.
 __device__ __forceinline__ int split_len(int kv, int n_splits) {
   const int even = (int)(((int64_t)kv + n_splits - 1) / n_splits);
-  return max(kStage, (even + kStage - 1) / kStage * kStage);
+  return max(2 * kStage, (even + kStage - 1) / kStage * kStage);
 }
 
 // One sequence and KV head as a workgroup sees it.
@@ -558,6 +559,9 @@ constexpr int kWant = 1024;
 // The same where a sequence has more than 64 (row, query head) pairs of a KV head: one a CU, and
 // parts of 1024 keys at least (500 rows of a prompt: 16 us in one part, 22 in two; 1000: 28, 45).
 constexpr int kWantMany = 256, kPartMany = 1024;
+// Keys of a part at least elsewhere: 256, or 128 where that leaves CUs without work (16 rows over
+// 8208 keys: 18 us in parts of 256, 23 of 128; over 2064 keys: 14.8 and 13.3).
+constexpr int kPart = 256, kPartFew = 128;
 // Rows of a workgroup of each shape.  The smallest shape that holds a sequence's rows is taken, so
 // that its keys are read once; the last one from 256 workgroups on (1000 rows of a prompt, 250 of them:
 // 28 us with the third, 37 with the last).
@@ -572,7 +576,8 @@ PagedAttnPlan paged_attention_plan(const sbd_paged_kv& c, int batch, int rows, i
   p.rowblocks = pairs / tr + batch;
   const int64_t groups = std::max<int64_t>(1, batch * ((each + tr - 1) / tr) * c.n_kv_heads);
   const bool many = each > 64;
-  const int64_t want = ((many ? kWantMany : kWant) + groups - 1) / groups, part = many ? kPartMany : kStage;
+  const int64_t want = ((many ? kWantMany : kWant) + groups - 1) / groups;
+  const int64_t part = many ? kPartMany : groups * ((max_kv + kPart - 1) / kPart) >= 256 ? kPart : kPartFew;
   p.n_splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, 64, (max_kv + part - 1) / part}));
   if (p.n_splits > 1) {
     const size_t items = (size_t)p.n_splits * rows * n_q;

@@ -91,15 +91,13 @@ class PagedStep:
         self._set(table, page_size, rows, p + 4 * rows, p + 4 * (rows + batch + 1), p)
         return self
 
-    def __getattr__(self, name):  # the views of a planned step are made when they are asked for
+    def __getattr__(self, name):  # the views of a planned step are made when one is asked for
         buf = self.__dict__.get("buf")
         if buf is None or name not in ("row_start", "kv_len", "slots"):
             raise AttributeError(name)
         r, b = self.rows, self.batch
-        at, n = {"slots": (0, r), "row_start": (r, b + 1), "kv_len": (r + b + 1, b)}[name]
-        t = buf[at:at + n]
-        self.__dict__[name] = t
-        return t
+        self.slots, self.row_start, self.kv_len, _ = buf.split_with_sizes((r, b + 1, b, buf.numel() - r - 2 * b - 1))
+        return self.__dict__[name]
 
 
 class PageTable:
