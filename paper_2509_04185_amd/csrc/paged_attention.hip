@@ -93,17 +93,28 @@ __device__ __forceinline__ int split_len(int kv, int n_splits) {
 struct Seq {
   int b, r0, n, kv, nc;
   int g, G, pshift;
+  int64_t block;  // the workgroup's among the sequence's row blocks
 };
-__device__ __forceinline__ Seq load_seq(const PagedAttnArgs& a, int b, int g) {
+// The sequence of row block `block` of tr rows: every row_start[b] * G / tr + b begins one.  What
+// is known about up to 64 sequences is read at once, before it is known which of them it is.
+__device__ __forceinline__ Seq find_seq(const PagedAttnArgs& a, int64_t block, int tr, int g) {
   Seq q;
-  q.b = b;
   q.g = g;
   q.G = a.n_q / a.c.n_kv_heads;
   q.pshift = 31 - __builtin_clz(a.c.page_size);
-  q.r0 = a.row_start[b];
-  q.n = a.row_start[b + 1] - q.r0;
-  q.kv = min(max(a.kv_len[b], 0), a.max_pages << q.pshift);
-  q.nc = a.n_causal ? a.n_causal[b] : q.n;
+  auto start = [&](int r0, int b) { return (int64_t)r0 * q.G / tr + b; };
+  int lo = 0, n = a.batch;
+  narrow_sequence(lo, n, 64, block, [&](int b) { return start(a.row_start[b], b); });
+  const int lane = threadIdx.x & 63, mine = lo + min(lane, n - 1);
+  const int r0 = a.row_start[mine], r1 = a.row_start[mine + 1], kv = a.kv_len[mine];
+  const int nc = a.n_causal ? a.n_causal[mine] : INT32_MAX;
+  const int c = max(1, (int)__popcll(__ballot(lane < n && start(r0, mine) <= block))) - 1;
+  q.b = __builtin_amdgcn_readlane(mine, c);
+  q.r0 = __builtin_amdgcn_readlane(r0, c);
+  q.n = __builtin_amdgcn_readlane(r1, c) - q.r0;
+  q.kv = min(max(__builtin_amdgcn_readlane(kv, c), 0), a.max_pages << q.pshift);
+  q.nc = __builtin_amdgcn_readlane(nc, c);
+  q.block = block - start(q.r0, q.b);
   if (q.kv < q.n) q.kv = 0;  // not served: no row sees a key
   return q;
 }
@@ -431,17 +442,14 @@ __global__ __launch_bounds__(64 * RW, RW == 4 ? 2 : 1) void paged_attn_kernel(Pa
   __shared__ Unit s_unit[kUnits];
   __shared__ int s_kmax[RW];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = lane >> 4;
-  const int H = a.c.n_kv_heads, G = a.n_q / H;
+  const int H = a.c.n_kv_heads;
   const int g = blockIdx.x % H, item = blockIdx.x / H;
   const int split = item % a.plan.n_splits;
   const int rb_all = (int)(a.plan.rowblocks - 1 - item / a.plan.n_splits);  // the last rows, which see most keys, first
-  auto start = [&](int b) { return (int64_t)a.row_start[b] * G / TR + b; };
-  const int b = find_sequence(a.batch, rb_all, start);
-  const Seq sq = load_seq(a, b, g);
-  const int64_t rb = rb_all - start(b);
-  if (sq.r0 < 0 || sq.n <= 0 || rb < 0 || rb * TR >= (int64_t)sq.n * G) return;
+  const Seq sq = find_seq(a, rb_all, TR, g);
+  if (sq.r0 < 0 || sq.n <= 0 || sq.block < 0 || sq.block * TR >= (int64_t)sq.n * sq.G) return;
   Rows<T, DH, RT> rows;
-  rows.init(a, sq, rb * TR + 16 * RT * w);
+  rows.init(a, sq, sq.block * TR + 16 * RT * w);
   if (lane == 0) s_kmax[w] = rows.kmax;
   __syncthreads();
   int kmax = 0;
