@@ -183,36 +183,33 @@ __device__ __forceinline__ i32x8 load_frag(RowPair p, int c, int k) {
   return join8(lo, hi);
 }
 
+// Vectors at addresses that are aligned to their elements only (the memory unit takes them so).
+typedef f32x4 __attribute__((aligned(4))) f32x4_any;
+typedef i32x4 __attribute__((aligned(2))) i32x4_any;
+typedef i32x2 __attribute__((aligned(2))) i32x2_any;
+
 template <class T>
-__device__ __forceinline__ void store4(void* out, int64_t at, int n_left, bool vec, f32x4 v) {
+__device__ __forceinline__ void store4(void* out, int64_t at, int n_left, f32x4 v) {
   if constexpr (std::is_same_v<T, float>) {
     float* p = static_cast<float*>(out) + at;
-    if (vec && n_left >= 4) {
-      *(f32x4*)p = v;
+    if (n_left >= 4) {
+      *(f32x4_any*)p = v;
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 3; ++i)
         if (i < n_left) p[i] = v[i];
     }
   } else {
     uint16_t* p = static_cast<uint16_t*>(out) + at;
     const uint32_t lo = pack2<T>(v[0], v[1]), hi = pack2<T>(v[2], v[3]);
-    if (vec && n_left >= 4) {
-      *(i32x2*)p = i32x2{(int)lo, (int)hi};
+    if (n_left >= 4) {
+      *(i32x2_any*)p = i32x2{(int)lo, (int)hi};
     } else {
       if (n_left > 0) p[0] = (uint16_t)lo;
       if (n_left > 1) p[1] = (uint16_t)(lo >> 16);
       if (n_left > 2) p[2] = (uint16_t)hi;
-      if (n_left > 3) p[3] = (uint16_t)(hi >> 16);
     }
   }
-}
-
-// Rows of out may be stored four elements at a time.
-template <class T>
-__device__ __forceinline__ bool vec_ok(const MatmulArgs& a) {
-  constexpr int ES = std::is_same_v<T, float> ? 4 : 2;
-  return a.out_stride % 4 == 0 && (uintptr_t)a.out % (4 * ES) == 0;
 }
 
 // At most 16 MT rows: the weights' bytes are all there is.  A workgroup makes 16 NT columns of
@@ -266,7 +263,7 @@ __global__ __launch_bounds__(64 * KW) void skinny_kernel(MatmulArgs a) {
 #pragma unroll
     for (int u = 1; u < KW; ++u) v += s_acc[u][t][lane];
     const int row = 16 * (t % MT) + r, n = n0 + 16 * (t / MT) + 4 * grp;
-    if (row < a.m) store4<T>(a.out, row * a.out_stride + n, a.n - n, vec_ok<T>(a), v);
+    if (row < a.m) store4<T>(a.out, row * a.out_stride + n, a.n - n, v);
   }
 }
 
@@ -408,8 +405,8 @@ __global__ __launch_bounds__(64 * MW * NW, MW * NW >= 8 ? 1 : 2) void tile_kerne
   };
   // One block.  The products of a fragment are issued one after the other; while one runs, the
   // sums take in the one before it and the next fragment is read.  When the last row fragment
-  // is there (two fragments' products are still to come) turn() passes the barrier at which
-  // every wave is done with this buffer and the next block has landed in the other.
+  // is there (its own products are still to come) turn() passes the barrier at which every wave
+  // is done with this buffer and the next block has landed in the other.
   auto step = [&](int buf, const Begin& b, auto tail, auto&& fill, auto&& turn) {
     i32x8 x = b.x, x_next = x;
     float scale = b.sx, scale_next = 0.f;
@@ -480,8 +477,8 @@ __global__ __launch_bounds__(64 * MW * NW, MW * NW >= 8 ? 1 : 2) void tile_kerne
     step(0, b, part, [](int) {}, [] {});
   }
 
-  // Each wave turns its sums around in a part of LDS of its own, so that it stores whole lines:
-  // 8-byte pieces of 16 rows straight from the registers cost 31 us a 256 x 256 tile.
+  // Each wave turns its sums around in a part of LDS of its own, so that it stores whole lines
+  // (4096 x 28672 x 4096: 517 us when measured, 543 with 8-byte pieces straight from the registers).
   using E = std::conditional_t<SPLIT, float, T>;
   constexpr int ES = std::is_same_v<E, float> ? 4 : 2, kWidth = 16 * NT * ES, kPieces = kWidth / 16;
   static_assert(S::BM * S::BN * ES <= (int)sizeof(s_x), "the sums fit the buffers");
@@ -504,7 +501,6 @@ __global__ __launch_bounds__(64 * MW * NW, MW * NW >= 8 ? 1 : 2) void tile_kerne
   asm volatile("" ::: "memory");
   uint8_t* out = static_cast<uint8_t*>(SPLIT ? static_cast<void*>(a.part + (int64_t)blockIdx.y * a.m * a.n) : a.out);
   const int64_t stride = SPLIT ? a.n : a.out_stride;
-  const bool vec = stride * ES % 16 == 0 && (uintptr_t)out % 16 == 0;
   constexpr int kRows = 64 / kPieces, kEls = 16 / ES;
   const int p = lane % kPieces, n = n0 + 16 * NT * nw + p * kEls;
 #pragma unroll
@@ -513,11 +509,11 @@ __global__ __launch_bounds__(64 * MW * NW, MW * NW >= 8 ? 1 : 2) void tile_kerne
     const i32x4 v = *(const i32x4*)(turn + row * kWidth + ((p ^ (row % kPieces)) * 16));
     if (m >= a.m || n >= a.n) continue;
     uint8_t* at = out + (m * stride + n) * ES;
-    if (vec && n + kEls <= a.n) {
-      *(i32x4*)at = v;
+    if (n + kEls <= a.n) {
+      *(i32x4_any*)at = v;
     } else {
 #pragma unroll
-      for (int e = 0; e < kEls; ++e) {
+      for (int e = 0; e < kEls - 1; ++e) {
         if (n + e >= a.n) break;
         if constexpr (ES == 4)
           *(int*)(at + 4 * e) = v[e];
@@ -538,15 +534,15 @@ __global__ __launch_bounds__(256) void join_splits_kernel(MatmulArgs a, int spli
   const float* p = a.part + (int64_t)row * a.n + n;
   f32x4 v{0.f, 0.f, 0.f, 0.f};
   for (int s = 0; s < splits; ++s, p += size) {
-    if (a.n % 4 == 0) {
-      v += *(const f32x4*)p;
+    if (left >= 4) {
+      v += *(const f32x4_any*)p;
     } else {
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
+      for (int q = 0; q < 3; ++q)
         if (q < left) v[q] += p[q];
     }
   }
-  store4<T>(a.out, row * a.out_stride + n, left, vec_ok<T>(a), v);
+  store4<T>(a.out, row * a.out_stride + n, left, v);
 }
 
 // How a product is cut.  Fewer tiles than CUs are split along K to two workgroups a CU (203 x 4096 x
@@ -560,15 +556,19 @@ struct MatmulPlan {
 static MatmulPlan matmul_plan(int m, int n, int k, bool wide) {
   MatmulPlan p{};
   const int kb = (k + 127) / 128;
-  // 32 x 4096 x 4096: 7.0 us with the first kernel, 10.7 with tiles; 32 x 28672 x 4096: 35 and 23.5
-  if (m <= 16 || (m <= 32 && n <= 8192)) {
+  // The first kernel and tiles: 32 x 4096 x 4096 6.3 and 10.7 us, 32 x 28672 x 4096 35 and 23.5; 64 x
+  // 4096 x 4096 10.2 and 13.0, 64 x 6144 x 4096 19 and 15, 40 x 4096 x 14336 30 and 20.
+  if (m <= 16 || (m <= 32 && n <= 8192) || (m <= 64 && n <= 4096 && k <= 4096)) {
     p.kind = MatmulPlan::kSkinny;
     p.splits = 1;
     return p;
   }
   auto tiles = [&](int bm, int bn) { return (int64_t)((m + bm - 1) / bm) * ((n + bn - 1) / bn); };
   int bm, bn;
-  if (!wide && tiles(256, 256) >= 192) {
+  // 256 x 256 where their rounds over the CUs are at least 5/8 full: 4096 x 6144 x 4096 (3/4) 124 us,
+  // 149 with 128 x 128; 2560 x 7168 x 4096 (0.55) 113 and 114; 2529 x 6454 x 320 (0.49) 25.5 and 19.5.
+  const int64_t round = (int64_t)256 * 256 * 256, rounds = (tiles(256, 256) + 255) / 256;
+  if (!wide && (int64_t)m * n >= rounds * round / 8 * 5) {
     p.kind = MatmulPlan::kLarge;
     bm = bn = 256;
   } else if (m > 64 && tiles(128, 128) >= 128) {
@@ -599,12 +599,17 @@ static hipError_t launch_skinny(const MatmulArgs& a, hipStream_t s) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)((a.n + 16 * nt - 1) / (16 * nt))), dim3(64 * kw), 0, s, a);
   };
   // few columns: narrow tiles and more waves along K, so that more CUs bring weights (16 x 4096 x
-  // 4096: 5.2 us with eight waves, 7.1 with four); many: two tiles a wave halve the reads of the rows
-  const bool two = a.n >= 8192;
-  if (a.m <= 16)
-    two ? go(skinny_kernel<T, 1, 2, 4>, 2, 4) : go(skinny_kernel<T, 1, 1, 8>, 1, 8);
+  // 4096: 4.6 us with sixteen waves, 5.2 with eight, 7.1 with four; 16 x 6144 x 4096: 9.7, 9.0); many:
+  // two tiles a wave halve the reads of the rows
+  const bool few = a.n <= 4096;
+  if (a.m > 32)
+    go(skinny_kernel<T, 4, 1, 8>, 1, 8);
+  else if (a.m > 16)
+    few ? go(skinny_kernel<T, 2, 1, 16>, 1, 16) : go(skinny_kernel<T, 2, 1, 8>, 1, 8);
+  else if (a.n >= 8192)
+    go(skinny_kernel<T, 1, 2, 4>, 2, 4);
   else
-    two ? go(skinny_kernel<T, 2, 2, 4>, 2, 4) : go(skinny_kernel<T, 2, 1, 8>, 1, 8);
+    few ? go(skinny_kernel<T, 1, 1, 16>, 1, 16) : go(skinny_kernel<T, 1, 1, 8>, 1, 8);
   return hipGetLastError();
 }
 

@@ -44,7 +44,7 @@ def _tensor(t, what: str, dtype, shape, device=None):
     """t's address; a ValueError unless it is a contiguous CUDA tensor of that type and shape."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda or (device is not None and t.device != device):
         raise ValueError(f"{what}: expected a CUDA tensor" + (f" on {device}" if device is not None else ""))
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{what}: expected a contiguous {dtype} tensor of shape {tuple(shape)}, got "
                          f"{t.dtype} {tuple(t.shape)}")
     return t.data_ptr()

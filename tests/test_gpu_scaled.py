@@ -141,6 +141,34 @@ def test_matmul_large(m, n, k, dtype):
     assert share <= 1.0 and np.isfinite(got).all()
 
 
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("m", [18, 33, 47, 64])
+def test_matmul_few_rows_many_columns(m, dtype):
+    """Both sides of the widths and depths at which 17 to 64 rows change their kernel."""
+    check_matmul(m, 4096, 272, dtype)
+    check_matmul(m, 4099, 144, dtype)
+    check_matmul(m, 16, 4096, dtype)
+    check_matmul(m, 17, 4112, dtype)
+
+
+@pytest.mark.parametrize("m,n,k,dtype", [(3300, 4099, 144, FP), (3500, 4100, 656, BF), (2529, 6454, 320, FP)],
+                         ids=lambda v: str(v))
+def test_matmul_large_odd_widths(m, n, k, dtype):
+    """The rows of the output begin at every alignment of the type."""
+    test_matmul_large(m, n, k, dtype)
+
+
+def test_matmul_large_strided_output():
+    """256-row tiles into rows of a wider, oddly aligned output: nothing beside them is written."""
+    from paper_2509_04185_amd import scaled_matmul
+    a, sa, b, sb = make(3300, 3301, 144, 7)
+    plain = scaled_matmul(a, sa, b, sb)
+    wide = torch.full((3300, 3309), 5.0, dtype=BF, device=DEV)
+    scaled_matmul(a, sa, b, sb, out=wide[:, 3:3304])
+    assert torch.equal(wide[:, 3:3304], plain)
+    assert bool((wide[:, :3] == 5).all()) and bool((wide[:, 3304:] == 5).all())
+
+
 @pytest.mark.parametrize("m", [9, 70, 300])
 def test_matmul_strided_output(m):
     """Rows of a wider, oddly aligned output: nothing beside them is written."""
