@@ -83,13 +83,13 @@ __device__ __forceinline__ int block_exponent(float amax) {
 __device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
 // Largest b in [0, n) with start(b) <= idx, for a start() that rises and start(0) <= idx: 64
-// probes at a time, so one or two rounds of loads.  Every lane of the wave takes part.  Leaves
-// lo and n such that b is one of lo .. lo + n, n <= want (1 or 64).  They stay in range whatever
-// start() gives.
+// probes at a time.  Every lane of the wave takes part.  Leaves
+// lo and n such that b is one of lo .. lo + n, n <= 64, for the caller's own last round.  They stay
+// in range whatever start() gives.
 template <class F>
-__device__ __forceinline__ void narrow_sequence(int& lo, int& n, int want, int64_t idx, F&& start) {
+__device__ __forceinline__ void narrow_sequence(int& lo, int& n, int64_t idx, F&& start) {
   const int lane = threadIdx.x & 63;
-  while (n > want) {
+  while (n > 64) {
     const int step = (n + 63) / 64;
     const int at = lane * step;
     const bool below = at < n && start(lo + at) <= idx;
@@ -98,11 +98,4 @@ __device__ __forceinline__ void narrow_sequence(int& lo, int& n, int want, int64
     n = min(step, n - (c - 1) * step);
   }
 }
-template <class F>
-__device__ __forceinline__ int find_sequence(int n, int64_t idx, F&& start) {
-  int lo = 0;
-  narrow_sequence(lo, n, 1, idx, start);
-  return __builtin_amdgcn_readfirstlane(lo);
-}
-
 }  // namespace sbd

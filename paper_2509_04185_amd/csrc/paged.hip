@@ -251,21 +251,25 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a) {
   const int head = blockIdx.y >> 1;
   const bool values = blockIdx.y & 1;
   const int tid = threadIdx.x;
-  auto start = [&](int b) { return (int64_t)(a.row_start[b] / P) + 2 * b; };
-  const int b = find_sequence(a.batch, blockIdx.x, start);
-  const int r0 = a.row_start[b], n = min(a.row_start[b + 1], a.rows) - r0;
+  // Few dependent reads, since they are most of a small step's time: what is known about up to 64
+  // sequences is read before it is known which of them it is, and the rows before their page is.
+  auto start = [&](int r0, int b) { return (int64_t)(r0 / P) + 2 * b; };
+  int lo = 0, nb = a.batch;
+  narrow_sequence(lo, nb, blockIdx.x, [&](int b) { return start(a.row_start[b], b); });
+  const int lane = tid & 63, b = lo + min(lane, nb - 1);
+  const int from = a.row_start[b], to = min(a.row_start[b + 1], a.rows);
+  const int c = max(1, (int)__popcll(__ballot(lane < nb && start(from, b) <= (int64_t)blockIdx.x))) - 1;
+  const int r0 = __builtin_amdgcn_readlane(from, c), n = __builtin_amdgcn_readlane(to, c) - r0;
   if (r0 < 0 || n <= 0) return;
   const int slot0 = a.slots[r0];
   if (slot0 < 0) return;
   // rows [j, j + m) of the sequence go to one page, from offset off
-  const int64_t chunk = blockIdx.x - start(b);
+  const int64_t chunk = blockIdx.x - start(r0, lo + c);
   const int lead = P - slot0 % P;  // rows that the first page still takes
   const int64_t j64 = chunk == 0 ? 0 : lead + (chunk - 1) * P;
   if (chunk < 0 || j64 >= n) return;
   const int j = (int)j64, m = min(n - j, chunk == 0 ? lead : P);
-  const int slot = a.slots[r0 + j];
-  const int page = slot / P, off = slot % P;
-  if (slot < 0 || page >= a.c.n_pages || off + m > P) return;
+  const int slot = chunk == 0 ? slot0 : a.slots[r0 + j];
 
   const int64_t stride = values ? a.v_stride : a.k_stride;
   const uint16_t* x = static_cast<const uint16_t*>(values ? a.v : a.k) + (int64_t)(r0 + j) * stride + (int64_t)head * DH;
@@ -275,6 +279,13 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a) {
   i32x4 hold[kHold];
   float amax = 0.f;
   auto piece = [&](int i) { return ld16(x + (int64_t)(i / kPieces) * stride + (i % kPieces) * 8); };
+#pragma unroll
+  for (int h = 0; h < kHold; ++h)
+    if (tid + h * kAppendThreads < m * kPieces) hold[h] = piece(tid + h * kAppendThreads);
+  const int page = slot / P, off = slot % P;
+  if (slot < 0 || page >= a.c.n_pages || off + m > P) return;
+  int8_t* exp = (values ? a.c.v_exp : a.c.k_exp) + (int64_t)page * H + head;
+  const int old = off > 0 ? *exp : 0;
   auto largest = [&](i32x4 w) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
@@ -284,13 +295,8 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a) {
   };
 #pragma unroll
   for (int h = 0; h < kHold; ++h)
-    if (tid + h * kAppendThreads < m * kPieces) hold[h] = piece(tid + h * kAppendThreads);
-#pragma unroll
-  for (int h = 0; h < kHold; ++h)
     if (tid + h * kAppendThreads < m * kPieces) largest(hold[h]);
   for (int i = tid + kHold * kAppendThreads; i < m * kPieces; i += kAppendThreads) largest(piece(i));
-  int8_t* exp = (values ? a.c.v_exp : a.c.k_exp) + (int64_t)page * H + head;
-  const int old = *exp;
   int e = block_exponent(block_max(amax));  // its barrier: every thread has read the old exponent
   if (off > 0) e = max(e, old);
   const bool grown = off > 0 && e > old;

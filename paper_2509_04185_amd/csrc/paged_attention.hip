@@ -104,7 +104,7 @@ __device__ __forceinline__ Seq find_seq(const PagedAttnArgs& a, int64_t block, i
   q.pshift = 31 - __builtin_clz(a.c.page_size);
   auto start = [&](int r0, int b) { return (int64_t)r0 * q.G / tr + b; };
   int lo = 0, n = a.batch;
-  narrow_sequence(lo, n, 64, block, [&](int b) { return start(a.row_start[b], b); });
+  narrow_sequence(lo, n, block, [&](int b) { return start(a.row_start[b], b); });
   const int lane = threadIdx.x & 63, mine = lo + min(lane, n - 1);
   const int r0 = a.row_start[mine], r1 = a.row_start[mine + 1], kv = a.kv_len[mine];
   const int nc = a.n_causal ? a.n_causal[mine] : INT32_MAX;

@@ -26,16 +26,18 @@ import torch
 from .binding import PagedKVArgs, PageTableArgs, _check, load_library
 
 TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}  # SBD_TYPE_*
+_HALVES = (torch.bfloat16, torch.float16)
+_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream  # no objects made on the way
 
 
 def _run(fn, device: torch.device, where: str, *args):
     """fn(stream, *args) with the tensors' device as the current one, on torch's current stream of it."""
     index = device.index
-    if index == torch._C._cuda_getDevice():
-        st = fn(torch._C._cuda_getCurrentRawStream(index), *args)
+    if index == _device():
+        st = fn(_raw_stream(index), *args)
     else:
         with torch.cuda.device(index):
-            st = fn(torch._C._cuda_getCurrentRawStream(index), *args)
+            st = fn(_raw_stream(index), *args)
     if st != 0:
         _check(load_library(), st, where)
 
@@ -51,15 +53,16 @@ def _tensor(t, what: str, dtype, shape, device=None):
 
 
 def _rows(t, what: str, heads: int, dim: int, device):
-    """Address and row stride of [rows][heads][dim] whose rows may lie apart."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != device:
+    """Address and row stride of [rows][heads][dim] on `device` (a CUDA one) whose rows may lie apart."""
+    if not isinstance(t, torch.Tensor) or t.device != device:
         raise ValueError(f"{what}: expected a CUDA tensor on {device}")
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.dtype not in (torch.bfloat16, torch.float16):
-        raise ValueError(f"{what}: expected bfloat16 or float16 [rows][{heads}][{dim}], got {t.dtype} {tuple(t.shape)}")
-    stride = t.stride()
-    if t.shape[0] and (stride[2] != 1 or (heads > 1 and stride[1] != dim)):
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[1] != heads or shape[2] != dim or t.dtype not in _HALVES:
+        raise ValueError(f"{what}: expected bfloat16 or float16 [rows][{heads}][{dim}], got {t.dtype} {tuple(shape)}")
+    n = shape[0]
+    if n and (stride[2] != 1 or (heads > 1 and stride[1] != dim)):
         raise ValueError(f"{what}: the heads of a row must be contiguous (strides {stride})")
-    return t.data_ptr(), (stride[0] if t.shape[0] > 1 else heads * dim)
+    return t.data_ptr(), (stride[0] if n > 1 else heads * dim)
 
 
 class PagedStep:
@@ -185,9 +188,8 @@ class PagedKV:
         pk, sk = _rows(k, "k", self.n_kv_heads, self.head_dim, self.device)
         pv, sv = _rows(v, "v", self.n_kv_heads, self.head_dim, self.device)
         self._step(step, k, "k")
-        self._step(step, v, "v")
-        if k.dtype != v.dtype:
-            raise ValueError("k and v have different types")
+        if k.shape != v.shape or k.dtype != v.dtype:
+            raise ValueError(f"k and v differ: {k.dtype} {tuple(k.shape)} and {v.dtype} {tuple(v.shape)}")
         _run(self.lib.sbd_paged_append, self.device, "sbd_paged_append", self._p, TYPES[k.dtype], step.batch, step.rows,
              step.p_row_start, step.p_slots, pk, sk, pv, sv)
 
