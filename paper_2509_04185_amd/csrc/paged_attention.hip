@@ -72,6 +72,9 @@ __device__ __forceinline__ float max_of_groups(float v) {
   return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
 }
 
+// The larger of m and x, m where x is NaN (m is not).  fmaxf would first quiet x by an instruction of its own.
+__device__ __forceinline__ float larger(float m, float x) { return __builtin_amdgcn_fmed3f(m, x, INFINITY); }
+
 // A run of 16 keys: where its page's codes of this KV head begin (page 0's where the table names
 // none: page is -1 then) and its exponents.
 struct Unit {
@@ -269,7 +272,8 @@ struct Rows {
     // s[t][u][i]: key run + 4 u + i of row r.  Keys that some row does not see need care: their
     // scores here, and their values where those are NaN.
     const bool edge = __any(ks + kStage > kmin || !known);
-    if (edge) {
+    if (__builtin_expect(edge, 0)) {
+      asm volatile("");  // a branch, not selects in every stage
 #pragma unroll
       for (int t = 0; t < RT; ++t)
 #pragma unroll
@@ -284,7 +288,9 @@ struct Rows {
     for (int t = 0; t < RT; ++t) {
       float top = -INFINITY;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) top = fmaxf(fmaxf(top, fmaxf(s[t][u][0], s[t][u][1])), fmaxf(s[t][u][2], s[t][u][3]));
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = larger(top, s[t][u][i]);
       top = max_of_groups(top * ke);
       mn[t] = top > m[t] + kSlack || m[t] == -INFINITY ? fmaxf(top, m[t]) : m[t];
       up |= mn[t] != m[t];
