@@ -437,9 +437,11 @@ __device__ __forceinline__ void store_out(const PagedAttnArgs& a, int row, int a
 // of workgroups on a CU, so LDS is kept small (36 KB at head_dim 128): with rings of four buffers
 // and half the workgroups 32 sequences x 8 rows x 2312 keys took 79 us instead of 48.  The keys
 // are split over workgroups where the rows do not fill the chip.  Where there are many rows two
-// tiles a wave share the conversion of the codes (3 prompts of 2500 rows: 341 us, one tile 365).
+// tiles a wave share the conversion of the codes (3 prompts of 2500 rows: 341 us, one tile 365).  The
+// bound of two waves a SIMD keeps the accumulators out of the other half of the registers (32 ragged
+// sequences: 47.9 us, 49.6 without).
 template <class T, int DH, int RT, int RW>
-__global__ __launch_bounds__(64 * RW, RW == 4 ? 2 : 1) void paged_attn_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(64 * RW, 2) void paged_attn_kernel(PagedAttnArgs a) {
   using L = Tiles<DH>;
   constexpr int NDT = DH / 16, TR = 16 * RT * RW, NB = 2;
   constexpr int kEach = L::kCopies / RW;  // copies of a wave and stage
