@@ -86,7 +86,7 @@ struct Unit {
 // Keys of a part: every sequence is split evenly, whatever lengths the call expected (parts of one
 // length for all, as long as the longest sequence needs: 32 sequences of 512 to 4104 keys 62 us
 // instead of 53, and twice that where the call did not know how long they are).  Two stages at
-// least: 4 sequences x 16 rows x 2016 keys take 28 us in 32 parts, 21 in 16.
+// least: 4 sequences x 16 rows x 2016 keys take 27 us in 32 parts, 19 in 8.
 __device__ __forceinline__ int split_len(int kv, int n_splits) {
   const int even = (int)(((int64_t)kv + n_splits - 1) / n_splits);
   return max(2 * kStage, (even + kStage - 1) / kStage * kStage);
@@ -437,7 +437,7 @@ __device__ __forceinline__ void store_out(const PagedAttnArgs& a, int row, int a
 // of workgroups on a CU, so LDS is kept small (36 KB at head_dim 128): with rings of four buffers
 // and half the workgroups 32 sequences x 8 rows x 2312 keys took 79 us instead of 48.  The keys
 // are split over workgroups where the rows do not fill the chip.  Where there are many rows two
-// tiles a wave share the conversion of the codes (3 prompts of 2500 rows: 341 us, one tile 365).  The
+// tiles a wave share the conversion of the codes (3 prompts of 2500 rows: 230 us, one tile 244).  The
 // bound of two waves a SIMD keeps the accumulators out of the other half of the registers (32 ragged
 // sequences: 47.9 us, 49.6 without).
 template <class T, int DH, int RT, int RW>
@@ -568,26 +568,27 @@ __global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a) {
     *out = (uint16_t)pack2<T>(acc[0] * inv, 0.f);
 }
 
-// Workgroups that a call is split into where it has fewer: four a CU.  Half as many leave CUs idle
-// behind ragged lengths (the 32 sequences above: 62 us), twice as many write and read more partial
-// outputs than they save (58 us).
+// Workgroups that a call is split into where it has fewer: four a CU.  Half as many are as fast where
+// lengths are equal (32 sequences x 8 rows x 2312 keys: 51 us, 50 with four a CU) and leave CUs
+// idle behind ragged ones; twice as many write and read more partial outputs than they save (57 us).
 constexpr int kWant = 1024;
 // The same where a sequence has more than 64 (row, query head) pairs of a KV head: one a CU, and
 // parts of 1024 keys at least (500 rows of a prompt: 16 us in one part, 22 in two; 1000: 28, 45).
 constexpr int kWantMany = 256, kPartMany = 1024;
 // Keys of a part at least elsewhere: 256, or 128 where that leaves CUs without work (16 rows over
-// 8208 keys: 18 us in parts of 256, 23 of 128; over 2064 keys: 14.8 and 13.3).
+// 8208 keys: 18 us in parts of 256, 23 of 128; over 2064 keys: 13.8 and 13.0).
 constexpr int kPart = 256, kPartFew = 128;
 // Rows of a workgroup of each shape.  The smallest shape that holds a sequence's rows is taken, so
-// that its keys are read once; the last one from 256 workgroups on (1000 rows of a prompt, 250 of them:
-// 28 us with the third, 37 with the last).
+// that its keys are read once; the last one from 512 workgroups on, two a CU (the third and the last:
+// a prompt of 1000 rows, 250 workgroups, 27 and 36 us; of 2500, 625, 89 and 84; of 4000, 1000, 197
+// and 182; 8 x 128 rows over 2128 keys, 256, 86 and 93; 16 x 128, 512, 118 and 100).
 static constexpr int kShapeRows[] = {16, 32, 64, 128};
 
 PagedAttnPlan paged_attention_plan(const sbd_paged_kv& c, int batch, int rows, int n_q, int max_kv) {
   PagedAttnPlan p{};
   const int64_t pairs = (int64_t)rows * (n_q / c.n_kv_heads);
   const int64_t each = (pairs + batch - 1) / batch;  // of a sequence, on average
-  p.shape = pairs / 128 * c.n_kv_heads >= 256 && each > 64 ? 3 : each <= 16 ? 0 : each <= 32 ? 1 : 2;
+  p.shape = pairs / 128 * c.n_kv_heads >= 512 && each > 64 ? 3 : each <= 16 ? 0 : each <= 32 ? 1 : 2;
   const int tr = kShapeRows[p.shape];
   p.rowblocks = pairs / tr + batch;
   const int64_t groups = std::max<int64_t>(1, batch * ((each + tr - 1) / tr) * c.n_kv_heads);

@@ -295,6 +295,14 @@ def test_attend_heads_and_masks(heads, group, dh, causal):
     check_attend(lens, 32, heads, group, dh, BF, causal, seed=group)
 
 
+@pytest.mark.parametrize("batch", [63, 64, 65, 130, 4200])
+def test_many_sequences(batch):
+    """More sequences than a wave looks at at once, some without rows."""
+    lens = [((7 * b) % 90, (5 * b) % 4) for b in range(batch)]
+    check_append(lens, 16, 1, 64, BF, seed=batch)
+    check_attend(lens, 16, 1, 2, 64, BF, "one", seed=batch)
+
+
 @pytest.mark.parametrize("lens", [[(0, 300)], [(37, 129), (0, 64), (900, 65)], [(0, 1), (0, 2), (3000, 40)]],
                          ids=lambda v: str(v))
 @pytest.mark.parametrize("dh", [64, 128])
